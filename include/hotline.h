@@ -59,7 +59,8 @@ typedef enum {
 #define HL_DEVERR_SHAPE 0x20u       /* bag_ptr[n_bags] differs from the n_lookups passed */
 #define HL_DEVERR_INTERNAL 0x40u    /* an internal bound check failed (never expected); the write was skipped */
 
-typedef enum { HL_F32 = 0, HL_BF16 = 1 } hl_dtype;
+/* HL_F16: rows of the routing calls and tensors of the clipping calls only */
+typedef enum { HL_F32 = 0, HL_BF16 = 1, HL_F16 = 2 } hl_dtype;
 
 typedef struct hl_handle hl_handle;
 typedef void* hl_stream; /* hipStream_t */
@@ -73,8 +74,8 @@ const char* hl_status_string(int32_t s);
  * each table's base (Sec. V-A "Data Dispatcher"; s_wr of the ISA table).
  * rows_per_table (host, n_tables entries) fixes gid = base[t] + row; total
  * rows must be < 2^32-1.  k_cap is the hot-cache capacity in rows (>= 1).
- * dtype is one of hl_dtype's values, passed as a plain int32 so that any value
- * a caller hands over is defined: any other value gives HL_ERR_INVALID_ARG.
+ * dtype is HL_F32 or HL_BF16, passed as a plain int32 so that any value a caller
+ * hands over is defined: any other value gives HL_ERR_INVALID_ARG.
  * Allocates the handle's device state on the current device: access counts
  * (4 B/row), hot-set bitmap (1 bit/row) and rank directory (4 B per 256 rows).
  * Synchronous. */
@@ -399,6 +400,135 @@ hl_status hl_embbag_bwd_apply_part(hl_handle* h, void* w_hot, void* staging, int
  * peer masks) if not; on != 0 makes every pass take the second form directly.
  * The grouping is the same either way. */
 hl_status hl_debug_ballot_ranks(hl_handle* h, int32_t on);
+
+/* ---------------------------------------------------------------- routing --
+ * Rows sent to experts and back: a token (a sample, a pooled bag, ...) goes to k
+ * experts, assignment a = t*k + j being token t's j-th.  hl_route_plan sorts the
+ * assignments by expert, as hl_partition sorts samples into two lists; the other
+ * calls move rows as the plan says: hl_route_gather copies a token's row to its
+ * assignments' places in the experts' blocks, hl_route_combine adds the experts'
+ * rows up at their tokens with the assignments' weights, and the two _bwd calls
+ * are their gradients.
+ *
+ * hl_route describes a plan (host struct, read during the call; its arrays are
+ * device memory of the caller).  An assignment is kept if its expert id is in
+ * [0, n_experts) and, with capacity > 0, fewer than capacity assignments before
+ * it (in ascending a) name its expert; an id -1 (padding) is never kept.  The
+ * plan writes
+ *   counts[e]  kept assignments of expert e            (n_experts entries)
+ *   offsets[e] first row of expert e's block, blocks of counts[e] rows rounded up
+ *              to a multiple of align one after another; offsets[n_experts] = the
+ *              rows in use                             (n_experts + 1 entries)
+ *   pos[a]     row of assignment a: offsets[its expert] + the kept assignments of
+ *              that expert before it; -1 if not kept   (n_tokens*k entries)
+ *   order[r]   the assignment in row r, -1 for the padding rows that round a block
+ *              up; rows from offsets[n_experts] on are left as they were
+ *                                                      (n_rows entries, or NULL)
+ * n_rows is the rows that order and every buffer of experts' rows hold, at least
+ * hl_route_rows(...): the most that any ids can use (0 for arguments out of
+ * range).  Integers only: the same ids always give the same plan.  An id outside
+ * [-1, n_experts) sets HL_DEVERR_OUT_OF_RANGE and is not kept.  n_tokens may be 0.
+ * Limits (HL_ERR_UNSUPPORTED): n_experts <= 1024, n_tokens*k <= 2^30, rows < 2^31.
+ * HL_ERR_CAPACITY: n_rows or the workspace (hl_route_workspace_bytes; any
+ * contents, NULL allowed where the call needs none: up to 8192 assignments) is
+ * too small.  The handle's device must be the current one. */
+typedef struct hl_route {
+  int64_t n_tokens;
+  int32_t k;
+  int32_t n_experts;
+  int32_t capacity; /* 0: none */
+  int32_t align;    /* >= 1 */
+  int64_t n_rows;
+  int32_t* counts;
+  int32_t* offsets;
+  int32_t* pos;
+  int32_t* order;
+} hl_route;
+int64_t hl_route_rows(int64_t n_tokens, int32_t k, int32_t n_experts, int32_t capacity, int32_t align);
+size_t hl_route_workspace_bytes(int64_t n_tokens, int32_t k, int32_t n_experts);
+hl_status hl_route_plan(hl_handle* h, const hl_route* r, const int32_t* experts, void* workspace, size_t ws_bytes,
+                        hl_stream stream);
+
+/* The row movements.  Rows hold dim elements of dtype (HL_F32, HL_BF16, HL_F16),
+ * stride elements apart (stride >= dim), at any address and stride that an
+ * element's alignment allows; the handle's tables play no part.  x, out, dout and
+ * dx are token rows [n_tokens], rows and drows experts' rows [n_rows]; weights and
+ * dweights are fp32 [n_tokens*k].  Outputs overlap no input.  Sums are held in
+ * fp32 and rounded once, to nearest even; their order is fixed.  An assignment
+ * that is not kept takes no part, whatever its weight holds: nothing is read or
+ * written for it but its dweights entry (0).  A token without kept assignments
+ * gets zeros (out, dx).  Rows that the plan does not use are left as they were.  A
+ * pos entry that is neither -1 nor below n_rows sets HL_DEVERR_BAD_CODE and is
+ * taken as not kept.
+ *   hl_route_gather       rows[pos[a]] = x[a / k]; padding rows = 0
+ *   hl_route_gather_bwd   dx[t] = sum over t's kept a of drows[pos[a]]
+ *   hl_route_combine      out[t] = sum over t's kept a of weights[a] rows[pos[a]]
+ *   hl_route_combine_bwd  drows[pos[a]] = weights[a] dout[a / k], padding rows 0;
+ *                         dweights[a] = dot(dout[a / k], rows[pos[a]])
+ * weights NULL: all 1.  dweights NULL: not computed (rows is then not read).
+ * gather and combine_bwd read counts and offsets too where align > 1. */
+hl_status hl_route_gather(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim, const void* x,
+                          int64_t x_stride, void* rows, int64_t rows_stride, hl_stream stream);
+hl_status hl_route_gather_bwd(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim, const void* drows,
+                              int64_t drows_stride, void* dx, int64_t dx_stride, hl_stream stream);
+hl_status hl_route_combine(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim, const void* rows,
+                           int64_t rows_stride, const float* weights, void* out, int64_t out_stride,
+                           hl_stream stream);
+hl_status hl_route_combine_bwd(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim, const void* dout,
+                               int64_t dout_stride, const void* rows, int64_t rows_stride, const float* weights,
+                               void* drows, int64_t drows_stride, float* dweights, hl_stream stream);
+
+/* --------------------------------------------------------------- clipping --
+ * A training step's global gradient norm and the clipped gradients.  The squares
+ * of the norm's parts are collected in an array sq of doubles (device), one entry
+ * per call that writes one: hl_grad_sq for a list of dense tensors,
+ * hl_embbag_bwd_norm for the tables of a handle (other ranks' entries may be
+ * gathered beside them).  The calls that clip take the whole array:
+ *   norm = sqrt(sq[0] + ... + sq[n_sq - 1])
+ *   c    = 1 if norm <= max_norm, else max_norm / norm; 0 if norm is not finite
+ * hl_grad (host struct, read during the call) is one tensor of n contiguous
+ * elements of dtype, at any address that an element's alignment allows; n may be
+ * 0, and n_grads too.
+ * hl_grad_sq: *sq = the sum of the squares of every src (dst is not read),
+ * squared and added in fp64 in an order that only the tensors' sizes fix.
+ * hl_grad_clip: dst = c * src, rounded once to nearest even; with c = 0 zeros,
+ * whatever src holds; dst = src (in place) or no overlap.  norm_out (device, may
+ * be NULL) receives the norm.  max_norm >= 0 (infinity: never above it).
+ * The tensors' addresses are read from the host array, which may be freed after
+ * the call; a captured graph keeps them.  The workspace (hl_grad_workspace_bytes)
+ * is zero-filled once before its first use (hl_workspace_init) and must not be
+ * one that holds a plan.  The handle's device must be the current one. */
+typedef struct hl_grad {
+  const void* src;
+  void* dst;
+  int64_t n;
+  int32_t dtype;
+} hl_grad;
+size_t hl_grad_workspace_bytes(void);
+hl_status hl_grad_sq(hl_handle* h, const hl_grad* grads, int32_t n_grads, double* sq, void* workspace, size_t ws_bytes,
+                     hl_stream stream);
+hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int32_t n_grads, const double* sq, int32_t n_sq,
+                       float max_norm, float* norm_out, hl_stream stream);
+
+/* hl_embbag_bwd_apply with clipping, in two halves on a plan's workspace.
+ * hl_embbag_bwd_norm reduces dY over each group (G_c as in hl_embbag_bwd_sgd),
+ * keeps the sums in the workspace and writes the sum of their squares, over every
+ * row of the plan, to *sq (device); it reads no embedding row.
+ * hl_embbag_bwd_clip then updates row(c) <- round_storage(row(c) - lr * c * G_c)
+ * from the kept sums (c as above; with c = 0 no row is written), bit for bit
+ * hl_embbag_bwd_apply with lr * c in place of lr (one fp32 product); norm_out as
+ * in hl_grad_clip.  Arguments as hl_embbag_bwd_apply's.  The norm needs a plan
+ * (made by hl_embbag_bwd_plan or hl_embbag_fwd_plan), the clipped update the norm
+ * on the same plan with no other call on that workspace in between, else
+ * HL_ERR_INVALID_ARG; it may be applied more than once (each a step with the same
+ * sums). */
+hl_status hl_embbag_bwd_norm(hl_handle* h, int32_t staging_rows, int32_t n_samples, int32_t bags_per_sample,
+                             int64_t n_lookups, const float* dY, double* sq, void* workspace, size_t ws_bytes,
+                             hl_stream stream);
+hl_status hl_embbag_bwd_clip(hl_handle* h, void* w_hot, void* staging, int32_t staging_rows, int32_t n_samples,
+                             int32_t bags_per_sample, int64_t n_lookups, const double* sq, int32_t n_sq,
+                             float max_norm, float lr, void* workspace, size_t ws_bytes, float* norm_out,
+                             hl_stream stream);
 
 /* ----------------------------------------------------------------- errors --
  * Waits for the device, returns the error word (HL_DEVERR_* bits) in *err_out

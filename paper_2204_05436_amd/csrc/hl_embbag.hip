@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "hl_embbag_fwd.h"
+#include "hl_grad.h"
 #include "hl_group_sort.h"
 #include "hl_internal.h"
 
@@ -111,6 +112,8 @@ struct bw_ws {
   uint32_t* tkey;    // [tiles]
   float* gc;         // [n_max][D] gradient sums of staging rows, kept between the two halves of the apply
   uint32_t* bnd;     // [1] first sorted position whose key is not a hot slot (set by the first half)
+  double* nsq;       // [nsq_max] sums of squares of the norm's blocks
+  size_t nsq_max;
   uint32_t tiles, gc_rows;
 };
 
@@ -143,6 +146,9 @@ static void bw_carve(hl_carver& c, bw_ws& ws, uint32_t n_max, int64_t max_bags, 
   ws.gc_rows = compact ? 0 : n_max;
   ws.gc = c.take<float>((size_t)ws.gc_rows * D);
   ws.bnd = c.take<uint32_t>(1);
+  // (a block per tile and 64 lanes of columns, and those of the second kernel: at most twice as many)
+  ws.nsq_max = compact ? 0 : 3 * ((size_t)ws.tiles + 1) * hl_div_up(D, 64);
+  ws.nsq = c.take<double>(ws.nsq_max);
   c.off = std::max(c.off, counts_end);
 }
 
@@ -237,22 +243,39 @@ __device__ __forceinline__ typename RowIO<VEC, BF>::T* bw_row(void* w_hot, void*
 #define GF_W 2u
 #define GF_L 4u
 
-// SPLIT: the run of a staging row (key n_hot + u, u < gc_rows) stores its sum
-// G in gc[u] instead of updating the row, and the row is not read; bw_cold
+// MODE BW_SPLIT: the run of a staging row (key n_hot + u, u < gc_rows) stores its
+// sum G in gc[u] instead of updating the row, and the row is not read; bw_cold
 // applies it later (the staging rows may still be in flight then).
+// MODE BW_NORM: every run stores its sum and no row is read or written.  The sum
+// lies in gc at the run's last position inside the group of RB_E positions where it
+// starts (its end, where it does not leave that group): a position that no other run
+// has, and that bw_clip recognises from the keys alone.  The sums' squares are added
+// up in fp64.
+#define BW_UPDATE 0
+#define BW_SPLIT 1
+#define BW_NORM 2
+template <int VEC>
+__device__ __forceinline__ double bw_square(const float* v) {
+  double s = 0.;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s = fma((double)v[e], (double)v[e], s);
+  return s;
+}
 __device__ __forceinline__ bool bw_deferred(uint32_t key, uint32_t n_hot, uint32_t gc_rows) {
   return key >= n_hot && key != EB_SENT && key - n_hot < gc_rows;
 }
 
-template <int VEC, bool BF, bool SPLIT>
+template <int VEC, bool BF, int MODE>
 __global__ void __launch_bounds__(RB_BLOCK)
 bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals, uint32_t n,
            const float* __restrict__ dY, eb_geom g, void* w_hot, void* stg, uint32_t n_hot, float lr,
            float* __restrict__ tfirst, float* __restrict__ tlast, uint32_t* __restrict__ tflag,
            uint32_t* __restrict__ tkey, float* __restrict__ gc, uint32_t gc_rows, uint32_t* __restrict__ bnd,
-           hl_hook hk) {
+           double* __restrict__ nsq, hl_hook hk) {
   typedef typename RowIO<VEC, BF>::T T;
   constexpr int RB_E = RB_EN(VEC);
+  constexpr bool SPLIT = MODE == BW_SPLIT;
+  double ss = 0.;
   __shared__ float pf[RB_WAVES * 64 * VEC], pl[RB_WAVES * 64 * VEC];
   hl_hook_head(hk);
   __shared__ uint32_t gflag[RB_WAVES * 64], gkey[RB_WAVES * 64];
@@ -313,7 +336,7 @@ bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals,
       if (j > 0 && valid && kk[j - 1] != kk[j]) from0 = false;
       const bool end = valid && (j == RB_E - 1 || kk[j + 1] != kk[j]);
       cpl[j] = end && !(from0 && cprev) && !(j == RB_E - 1 && cnext);
-      if (cpl[j] && cact && !(SPLIT && bw_deferred(kk[j], n_hot, gc_rows)))
+      if (MODE != BW_NORM && cpl[j] && cact && !(SPLIT && bw_deferred(kk[j], n_hot, gc_rows)))
         wr[j] = RowIO<VEC, BF>::load_raw(bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, kk[j]) + col);
     }
     float acc[VEC];
@@ -333,7 +356,10 @@ bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals,
       if (end) {
         if (cpl[j]) {
           if (cact) {
-            if (SPLIT && bw_deferred(kk[j], n_hot, gc_rows)) {
+            if (MODE == BW_NORM) {
+              st_f32<VEC>(gc + (int64_t)(e0 + j) * g.D + col, acc);
+              ss += bw_square<VEC>(acc);
+            } else if (SPLIT && bw_deferred(kk[j], n_hot, gc_rows)) {
               st_f32<VEC>(gc + (int64_t)(kk[j] - n_hot) * g.D + col, acc);
             } else {
               float wv[VEC], nw[VEC];
@@ -380,8 +406,14 @@ bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals,
         if (!(gflag[g2] & GF_W)) { done = true; break; }
       }
       const uint32_t key = gkey[grp];
+      const uint64_t at = tb + (uint64_t)grp * RB_E + RB_E - 1;  // the group's last position
       if (done) {
-        if (cact && SPLIT && bw_deferred(key, n_hot, gc_rows)) {
+        if (MODE == BW_NORM) {
+          if (cact) {
+            st_f32<VEC>(gc + (int64_t)at * g.D + col, acc);
+            ss += bw_square<VEC>(acc);
+          }
+        } else if (cact && SPLIT && bw_deferred(key, n_hot, gc_rows)) {
           st_f32<VEC>(gc + (int64_t)(key - n_hot) * g.D + col, acc);
         } else if (cact) {
           T* p = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, key) + col;
@@ -395,7 +427,7 @@ bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals,
         if (cact) st_f32<VEC>(tlast + (int64_t)tile * g.D + col, acc);
         if (gl == 0) {
           atomicOr(&s_tflag, GF_L);
-          if (blockIdx.y == 0) tkey[tile] = key;
+          if (blockIdx.y == 0) tkey[tile] = MODE == BW_NORM ? (uint32_t)at : key;
         }
       }
     }
@@ -419,6 +451,10 @@ bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals,
   }
   __syncthreads();
   if (threadIdx.x == 0 && blockIdx.y == 0) tflag[tile] = s_tflag;
+  if (MODE == BW_NORM) {
+    ss = hl_block_sum(ss);
+    if (threadIdx.x == 0) nsq[blockIdx.x + (size_t)gridDim.x * blockIdx.y] = ss;
+  }
   hl_hook_tail(hk);
 }
 
@@ -434,13 +470,13 @@ bw_reduce1(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals,
 // flag of tile a + 1 + this thread; s_end: n_tiles, in LDS, seen by every thread.
 // Nothing is done for one of at most `most` pieces.  Every thread of the block
 // calls it.
-template <int VEC, bool BF, bool SPLIT>
+template <int VEC, bool BF, int MODE>
 __device__ __forceinline__ void bw_reduce2_long(uint32_t t, uint32_t a, uint32_t f2, uint32_t* s_end, uint32_t most,
                                                 uint32_t n_tiles, eb_geom g, void* w_hot, void* stg,
                                                 uint32_t n_hot, float lr, const float* __restrict__ tfirst,
                                                 const float* __restrict__ tlast, const uint32_t* __restrict__ tflag,
                                                 const uint32_t* __restrict__ tkey, float* __restrict__ gc,
-                                                uint32_t gc_rows) {
+                                                uint32_t gc_rows, double* ss) {
   typedef typename RowIO<VEC, BF>::T T;
   __shared__ float part[RB_WAVES * 64 * VEC];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -464,7 +500,9 @@ __device__ __forceinline__ void bw_reduce2_long(uint32_t t, uint32_t a, uint32_t
   __syncthreads();
   uint32_t tend = *s_end;
   // the row, for group 0 (its address needs only the key)
-  const bool defer = SPLIT && bw_deferred(key, n_hot, gc_rows);
+  // (BW_NORM: key is the position of the sum)
+  const bool defer = MODE == BW_NORM || (MODE == BW_SPLIT && bw_deferred(key, n_hot, gc_rows));
+  const int64_t dst = (int64_t)(MODE == BW_NORM ? key : key - n_hot) * g.D + col;  // (where defer)
   typename RowIO<VEC, BF>::Raw wr;  // (unpacked when it is used)
   T* rp = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, key) + col;
   if (grp == 0 && cact && !defer) wr = RowIO<VEC, BF>::load_raw(rp);
@@ -521,7 +559,8 @@ __device__ __forceinline__ void bw_reduce2_long(uint32_t t, uint32_t a, uint32_t
 #pragma unroll
       for (int e = 0; e < VEC; ++e) acc[e] += part[(q * g.G + gl) * VEC + e];
     if (defer) {
-      st_f32<VEC>(gc + (int64_t)(key - n_hot) * g.D + col, acc);
+      st_f32<VEC>(gc + dst, acc);
+      if (MODE == BW_NORM) *ss += bw_square<VEC>(acc);
       return;
     }
     float wv[VEC];
@@ -559,12 +598,12 @@ __host__ __device__ __forceinline__ uint32_t bw_r2_blocks(uint32_t n_tiles, cons
   const uint32_t ngb = RB_WAVES * (uint32_t)g.NG;
   return bw_r2_longs(n_tiles, g) + (n_tiles + ngb - 1) / ngb;
 }
-template <int VEC, bool BF, bool SPLIT>
+template <int VEC, bool BF, int MODE>
 __device__ __forceinline__ void bw_reduce2_body(uint32_t bid, uint32_t n_tiles, eb_geom g, void* w_hot, void* stg,
                                                 uint32_t n_hot, float lr, const float* __restrict__ tfirst,
                                                 const float* __restrict__ tlast, const uint32_t* __restrict__ tflag,
                                                 const uint32_t* __restrict__ tkey, float* __restrict__ gc,
-                                                uint32_t gc_rows) {
+                                                uint32_t gc_rows, double* ss) {
   typedef typename RowIO<VEC, BF>::T T;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int gi = lane / g.G, gl = lane - gi * g.G;
@@ -591,8 +630,8 @@ __device__ __forceinline__ void bw_reduce2_body(uint32_t bid, uint32_t n_tiles, 
     for (int i = R2_SHORT - 1; i > 0; --i)
       if (i <= (int)step && !(fb[i] & GF_W)) back = i;
     if (back != 0)
-      bw_reduce2_long<VEC, BF, SPLIT>(a - back, a, f2, &s_end, most, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
-                                      gc_rows);
+      bw_reduce2_long<VEC, BF, MODE>(a - back, a, f2, &s_end, most, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
+                                     gc_rows, ss);
     return;
   }
   const uint32_t t = (bid - longs) * (uint32_t)ngb + grp;
@@ -621,7 +660,7 @@ __device__ __forceinline__ void bw_reduce2_body(uint32_t bid, uint32_t n_tiles, 
     for (int i = R2_SHORT - 2; i >= 0; --i)
       if (!(nf[i] & GF_W) || t + 1 + i == n_tiles - 1) np = i + 2;
     if (np != 0 && np <= most && cact) {
-      const bool defer = SPLIT && bw_deferred(key, n_hot, gc_rows);
+      const bool defer = MODE == BW_NORM || (MODE == BW_SPLIT && bw_deferred(key, n_hot, gc_rows));
       T* rp = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, key) + col;
       float wv[VEC];
       if (!defer) RowIO<VEC, BF>::load(rp, wv);
@@ -636,7 +675,8 @@ __device__ __forceinline__ void bw_reduce2_body(uint32_t bid, uint32_t n_tiles, 
         for (int e = 0; e < VEC; ++e) acc[e] += v[e];
       }
       if (defer) {
-        st_f32<VEC>(gc + (int64_t)(key - n_hot) * g.D + col, acc);
+        st_f32<VEC>(gc + (int64_t)(MODE == BW_NORM ? key : key - n_hot) * g.D + col, acc);
+        if (MODE == BW_NORM) *ss += bw_square<VEC>(acc);
       } else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) wv[e] -= lr * acc[e];
@@ -646,13 +686,92 @@ __device__ __forceinline__ void bw_reduce2_body(uint32_t bid, uint32_t n_tiles, 
   }
 }
 
-template <int VEC, bool BF, bool SPLIT>
+template <int VEC, bool BF, int MODE>
 __global__ void __launch_bounds__(RB_BLOCK)
 bw_reduce2(uint32_t n_tiles, eb_geom g, void* w_hot, void* stg, uint32_t n_hot, float lr,
            const float* __restrict__ tfirst, const float* __restrict__ tlast, const uint32_t* __restrict__ tflag,
            const uint32_t* __restrict__ tkey, float* __restrict__ gc, uint32_t gc_rows) {
-  bw_reduce2_body<VEC, BF, SPLIT>(blockIdx.x, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
-                                  gc_rows);
+  bw_reduce2_body<VEC, BF, MODE>(blockIdx.x, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
+                                  gc_rows, nullptr);
+}
+
+// The norm's second kernel: the segments that span tiles, and the sum of every
+// block's squares (the first kernel's n1 at nsq, this one's behind them, each block
+// with its share of the first's).
+template <int VEC, bool BF>
+__global__ void __launch_bounds__(RB_BLOCK)
+bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const float* __restrict__ tlast,
+         const uint32_t* __restrict__ tflag, const uint32_t* __restrict__ tpos, float* __restrict__ gc, double* nsq,
+         uint32_t n1, uint32_t* ticket, double* __restrict__ out, uint32_t* err) {
+  double ss = 0., total;
+  bw_reduce2_body<VEC, BF, BW_NORM>(blockIdx.x, n_tiles, g, nullptr, nullptr, 0, 0.f, tfirst, tlast, tflag, tpos, gc, 0,
+                                    &ss);
+  const uint32_t n2 = gridDim.x * gridDim.y, bid = blockIdx.x + gridDim.x * blockIdx.y;
+  const uint32_t i0 = (uint32_t)((uint64_t)bid * n1 / n2), i1 = (uint32_t)((uint64_t)(bid + 1) * n1 / n2);
+  for (uint32_t i = i0 + threadIdx.x; i < i1; i += RB_BLOCK) ss += nsq[i];
+  __syncthreads();
+  if (hl_grid_sum(ss, nsq + n1, ticket, n2, err, &total)) *out = total;
+}
+
+// The clipped update from the sums that the norm kept: every position that holds
+// one (BW_NORM above; E positions per group) applies row <- round(row - lr * G), lr
+// scaled by the clipping coefficient.  A wave tests BC_POS positions, lists those
+// found in LDS, and its row groups take them RPG at a time, all loads in flight
+// together.
+#define BC_POS 64
+template <int VEC, bool BF>
+__global__ void __launch_bounds__(256)
+bw_clip(const uint32_t* __restrict__ keys, uint32_t n, uint32_t E, eb_geom g, void* w_hot, void* stg, uint32_t n_hot,
+        float lr, const float* __restrict__ gc, const double* __restrict__ sq, int32_t n_sq, float max_norm,
+        float* __restrict__ norm_out) {
+  typedef typename RowIO<VEC, BF>::T T;
+  constexpr int RPG = 4;
+  __shared__ uint2 s_at[4][BC_POS];
+  float norm;
+  const float coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
+  if (norm_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *norm_out = norm;
+  if (coef == 0.f) return;
+  lr *= coef;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int gi = lane / g.G, gl = lane - gi * g.G;
+  const int32_t colv = blockIdx.y * 64 + gl;
+  const bool cact = gi < g.NG && colv < g.vpr;
+  const int64_t col = (int64_t)colv * VEC;
+  const uint64_t p = ((uint64_t)blockIdx.x * 4 + w) * BC_POS + lane;
+  uint32_t key = EB_SENT;
+  bool mine = false;
+  if (p < n) {
+    key = keys[p];
+    const uint32_t r = (uint32_t)(p % E);
+    const uint32_t next = p + 1 < n ? keys[p + 1] : EB_SENT, before = p > r ? keys[p - r - 1] : EB_SENT;
+    mine = key != EB_SENT && (r == E - 1 || next != key) && before != key;
+  }
+  const uint64_t m = __ballot(mine);
+  if (mine) s_at[w][__popcll(m & ((1ull << lane) - 1ull))] = make_uint2((uint32_t)p, key);
+  const int cnt = __popcll(m);
+  __syncthreads();
+  for (int i0 = 0; i0 < cnt; i0 += RPG * g.NG) {
+    T* row[RPG];
+    float wv[RPG][VEC], gv[RPG][VEC];
+#pragma unroll
+    for (int j = 0; j < RPG; ++j) {
+      const int i = i0 + j * g.NG + gi;
+      row[j] = nullptr;
+      if (i < cnt && cact) {
+        const uint2 a = s_at[w][i];
+        row[j] = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, a.y) + col;
+        RowIO<VEC, BF>::load(row[j], wv[j]);
+        ld_f32<VEC>(gc + (int64_t)a.x * g.D + col, gv[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < RPG; ++j)
+      if (row[j]) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) wv[j][e] = wv[j][e] - lr * gv[j][e];
+        RowIO<VEC, BF>::store(row[j], wv[j]);
+      }
+  }
 }
 
 // The deferred staging-row updates: every run end in the sorted keys whose key
@@ -854,8 +973,8 @@ eb_tail_r2(uint32_t n_tiles, void* w_hot, uint32_t n_hot, float lr, const float*
            float* __restrict__ out, uint32_t* err) {
   const uint32_t r2 = bw_r2_blocks(n_tiles, g);
   if (blockIdx.x < r2) {
-    bw_reduce2_body<VEC, BF, true>(blockIdx.x, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
-                                   gc_rows);
+    bw_reduce2_body<VEC, BF, BW_SPLIT>(blockIdx.x, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
+                                       gc_rows, nullptr);
     return;
   }
   eb_tail_body<VEC, BF, RB_WAVES>(blockIdx.x - r2, gridDim.x - r2, keys, vals, n, bnd, g, stg, stg_rows,
@@ -875,8 +994,8 @@ eb_bags_r2(uint32_t n_tiles, void* w_hot, uint32_t n_hot, float lr, const float*
            float* __restrict__ out, uint32_t* err) {
   const uint32_t r2 = bw_r2_blocks(n_tiles, g);
   if (blockIdx.x < r2) {
-    bw_reduce2_body<VEC, BF, true>(blockIdx.x, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
-                                   gc_rows);
+    bw_reduce2_body<VEC, BF, BW_SPLIT>(blockIdx.x, n_tiles, g, w_hot, stg, n_hot, lr, tfirst, tlast, tflag, tkey, gc,
+                                       gc_rows, nullptr);
     return;
   }
   eb_fwd_body<VEC, BF, 2>(blockIdx.x - r2, gridDim.x - r2, w_hot, stg, stg_rows, n_hot, k_cap, codes,
@@ -1005,16 +1124,17 @@ static void launch_bwd(const hl_handle* h, uint32_t tiles, hipStream_t s, const 
                        bw_ws& ws, int part) {
   const dim3 grid(tiles, g.cchunks), grid2(bw_r2_blocks(tiles, g), g.cchunks);
   if (part == 0) {
-    HL_KERNEL(h, s, "bw_reduce1", (bw_reduce1<VEC, BF, false>), grid, dim3(RB_BLOCK), 0, s, sk, sv, n, dY, g,
-              w_hot, stg, n_hot, lr, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows, ws.bnd, hl_hook{});
-    HL_KERNEL(h, s, "bw_reduce2", (bw_reduce2<VEC, BF, false>), grid2, dim3(RB_BLOCK), 0, s, tiles, g, w_hot, stg,
+    HL_KERNEL(h, s, "bw_reduce1", (bw_reduce1<VEC, BF, BW_UPDATE>), grid, dim3(RB_BLOCK), 0, s, sk, sv, n, dY, g,
+              w_hot, stg, n_hot, lr, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows, ws.bnd, nullptr,
+              hl_hook{});
+    HL_KERNEL(h, s, "bw_reduce2", (bw_reduce2<VEC, BF, BW_UPDATE>), grid2, dim3(RB_BLOCK), 0, s, tiles, g, w_hot, stg,
               n_hot, lr, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows);
   } else if (part == 1 || part == 3) {
-    HL_KERNEL(h, s, "bw_reduce1", (bw_reduce1<VEC, BF, true>), grid, dim3(RB_BLOCK), 0, s, sk, sv, n, dY, g,
-              w_hot, stg, n_hot, lr, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows, ws.bnd,
+    HL_KERNEL(h, s, "bw_reduce1", (bw_reduce1<VEC, BF, BW_SPLIT>), grid, dim3(RB_BLOCK), 0, s, sk, sv, n, dY, g,
+              w_hot, stg, n_hot, lr, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows, ws.bnd, nullptr,
               part == 3 ? hl_hook_take(h) : hl_hook{});
     if (part == 1)
-      HL_KERNEL(h, s, "bw_reduce2", (bw_reduce2<VEC, BF, true>), grid2, dim3(RB_BLOCK), 0, s, tiles, g, w_hot, stg,
+      HL_KERNEL(h, s, "bw_reduce2", (bw_reduce2<VEC, BF, BW_SPLIT>), grid2, dim3(RB_BLOCK), 0, s, tiles, g, w_hot, stg,
                 n_hot, lr, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows);
   } else {
     // the tail (cold lookups: about a tenth of a mini-batch here) is a part of
@@ -1277,6 +1397,99 @@ hl_status hl_embbag_bwd_apply_any(hl_handle* h, void* w_hot, void* staging, int3
     rec->part1 = part == 1 ? 1 : 3;
     rec->vec = vec;
   }
+  return HL_OK;
+}
+
+// What the two halves of the clipped update share: the plan's record, its
+// workspace and its sorted pairs (pass: the record's state that the call needs).
+static hl_status norm_setup(hl_handle* h, int32_t stg_rows, int32_t n_samples, int32_t bps, int64_t n_lookups,
+                            void* workspace, size_t ws_bytes, hl_ws_rec** rec, bw_ws* ws, uint32_t** sk,
+                            uint32_t** sv) {
+  if (!h || n_samples < 0 || bps < 1 || n_lookups < 0 || stg_rows < 0 || !workspace) return HL_ERR_INVALID_ARG;
+  const int64_t n_bags = (int64_t)n_samples * bps;
+  *rec = hl_ws_find(h, workspace);
+  if (!*rec || (*rec)->n != n_lookups || (*rec)->bags != n_bags || (*rec)->stg != stg_rows || (*rec)->compact ||
+      (*rec)->n_hot != h->n_hot)
+    return HL_ERR_INVALID_ARG;  // no matching plan is held by this workspace
+  if (ws_bytes < bw_bytes(h, n_lookups, n_bags, false)) return HL_ERR_CAPACITY;
+  hl_carver c = hl_carver::after_header(workspace, ws_bytes);
+  bw_carve(c, *ws, (uint32_t)n_lookups, n_bags, h->dim, false);
+  hl_sort_result(ws->sort, bw_key_bits(h, stg_rows), sk, sv);
+  return hl_on_device(h);
+}
+
+template <int VEC, bool BF>
+static void launch_norm(const hl_handle* h, uint32_t tiles, hipStream_t s, const uint32_t* sk, const uint32_t* sv,
+                        uint32_t n, const float* dY, eb_geom g, bw_ws& ws, uint32_t* ticket, double* sq) {
+  const dim3 grid(tiles, g.cchunks), grid2(bw_r2_blocks(tiles, g), g.cchunks);
+  HL_KERNEL(h, s, "bw_norm1", (bw_reduce1<VEC, BF, BW_NORM>), grid, dim3(RB_BLOCK), 0, s, sk, sv, n, dY, g, nullptr,
+            nullptr, h->n_hot, 0.f, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows, ws.bnd, ws.nsq, hl_hook{});
+  HL_KERNEL(h, s, "bw_norm2", (bw_norm2<VEC, BF>), grid2, dim3(RB_BLOCK), 0, s, tiles, g, ws.tfirst, ws.tlast, ws.tflag,
+            ws.tkey, ws.gc, ws.nsq, grid.x * grid.y, ticket, sq, h->d_err);
+}
+
+extern "C" hl_status hl_embbag_bwd_norm(hl_handle* h, int32_t stg_rows, int32_t n_samples, int32_t bps,
+                                        int64_t n_lookups, const float* dY, double* sq, void* workspace,
+                                        size_t ws_bytes, hl_stream stream) {
+  if (!sq || (uintptr_t)sq % 8 != 0) return HL_ERR_INVALID_ARG;
+  hl_ws_rec* rec;
+  bw_ws ws;
+  uint32_t *sk, *sv;
+  hl_status st = norm_setup(h, stg_rows, n_samples, bps, n_lookups, workspace, ws_bytes, &rec, &ws, &sk, &sv);
+  if (st != HL_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const int vec = eb_pick_vec(h->dim, h->dtype == HL_F32 ? 4 : 2, {dY});
+  if (rec->n == 0 || n_samples == 0) {
+    st = hl_fill32((uint32_t*)sq, 2, 0, s);
+  } else {
+    if (!dY) return HL_ERR_INVALID_ARG;
+    const eb_geom g = eb_make_geom(h->dim, vec);
+    const uint32_t n = (uint32_t)n_lookups, tiles = hl_div_up(n, bw_tile_entries(h->dim, vec));
+    if (tiles > ws.tiles || ((size_t)tiles + bw_r2_blocks(tiles, g)) * g.cchunks > ws.nsq_max) return HL_ERR_CAPACITY;
+    uint32_t* ticket = (uint32_t*)workspace + HL_HDR_GRAD;
+#define NORM(V, B) launch_norm<V, B>(h, tiles, s, sk, sv, n, dY, g, ws, ticket, sq)
+    if (vec == 8) NORM(8, true);  // (the type of the rows, which are not read, has no part in the others)
+    else if (vec == 4) NORM(4, false);
+    else if (vec == 2) NORM(2, false);
+    else NORM(1, false);
+#undef NORM
+    HL_LAUNCHED();
+  }
+  if (st != HL_OK) return st;
+  rec->part1 = 4;
+  rec->vec = vec;
+  return HL_OK;
+}
+
+extern "C" hl_status hl_embbag_bwd_clip(hl_handle* h, void* w_hot, void* staging, int32_t stg_rows, int32_t n_samples,
+                                        int32_t bps, int64_t n_lookups, const double* sq, int32_t n_sq, float max_norm,
+                                        float lr, void* workspace, size_t ws_bytes, float* norm_out,
+                                        hl_stream stream) {
+  if (!sq || (uintptr_t)sq % 8 != 0 || n_sq < 1 || !(max_norm >= 0.f) || (uintptr_t)norm_out % 4 != 0)
+    return HL_ERR_INVALID_ARG;
+  hl_ws_rec* rec;
+  bw_ws ws;
+  uint32_t *sk, *sv;
+  hl_status st = norm_setup(h, stg_rows, n_samples, bps, n_lookups, workspace, ws_bytes, &rec, &ws, &sk, &sv);
+  if (st != HL_OK) return st;
+  if (rec->part1 != 4) return HL_ERR_INVALID_ARG;  // the norm has not run on this plan
+  const bool none = rec->n == 0 || n_samples == 0;
+  if (!none && ((h->n_hot && !w_hot) || (stg_rows && !staging))) return HL_ERR_INVALID_ARG;
+  if (none && !norm_out) return HL_OK;
+  const int vec = eb_pick_vec(h->dim, h->dtype == HL_F32 ? 4 : 2, {w_hot, staging});
+  const eb_geom g = eb_make_geom(h->dim, vec);
+  const uint32_t n = none ? 0u : (uint32_t)n_lookups, E = RB_EN(rec->vec);
+  hipStream_t s = (hipStream_t)stream;
+  const bool bf = h->dtype == HL_BF16;
+#define CLIP(V, B)                                                                                                  \
+  HL_KERNEL(h, s, "bw_clip", (bw_clip<V, B>), dim3(n ? hl_div_up(n, 4 * BC_POS) : 1, g.cchunks), dim3(256), 0, s, sk, n, E, g, \
+            w_hot, staging, h->n_hot, lr, ws.gc, sq, n_sq, max_norm, norm_out)
+  if (vec == 8) CLIP(8, true);  // (bf16 only)
+  else if (vec == 4) { if (bf) CLIP(4, true); else CLIP(4, false); }
+  else if (vec == 2) { if (bf) CLIP(2, true); else CLIP(2, false); }
+  else { if (bf) CLIP(1, true); else CLIP(1, false); }
+#undef CLIP
+  HL_LAUNCHED();
   return HL_OK;
 }
 

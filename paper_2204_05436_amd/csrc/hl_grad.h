@@ -1,0 +1,73 @@
+// Sums over a grid in 64 bits and the clipping coefficient, shared by the dense
+// tensors' clipping (hl_grad.hip) and the tables' (hl_embbag.hip).
+#pragma once
+#include "hl_internal.h"
+
+__device__ __forceinline__ double hl_wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// The sum of v over the block, on thread 0, always in the same order.  Every
+// thread of a block of up to 1024 calls it.
+__device__ __forceinline__ double hl_block_sum(double v) {
+  __shared__ double s_part[16];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = (int)(blockDim.x >> 6);
+  v = hl_wave_sum(v);
+  if (lane == 0) s_part[w] = v;
+  __syncthreads();
+  double t = 0.;
+  if (threadIdx.x == 0)
+    for (int q = 0; q < nw; ++q) t += s_part[q];
+  __syncthreads();  // s_part is reused
+  return t;
+}
+
+// Adds up v over the grid's n blocks in block order: each publishes its sum in
+// part[block], and the taker of the last ticket adds them.  True on thread 0 of
+// that block, with the sum in *total.  A header that was not zero-filled, or that
+// overlapping calls share, hands out tickets past n: HL_DEVERR_INTERNAL.
+__device__ __forceinline__ bool hl_grid_sum(double v, double* part, uint32_t* ticket, uint32_t n, uint32_t* err,
+                                            double* total) {
+  __shared__ uint32_t s_last;
+  const uint32_t bid = blockIdx.x + gridDim.x * blockIdx.y;
+  v = hl_block_sum(v);
+  if (n == 1) {
+    *total = v;
+    return threadIdx.x == 0;
+  }
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(part + bid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __threadfence();  // the sum before the ticket
+    uint32_t epoch;
+    const uint32_t t = hl_ticket(ticket, n, &epoch);
+    if (t >= n) hl_flag(err, HL_DEVERR_INTERNAL);
+    s_last = t == n - 1;
+  }
+  __syncthreads();
+  if (!s_last) return false;
+  __threadfence();
+  double x = 0.;
+  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x)
+    x += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  *total = hl_block_sum(x);
+  return threadIdx.x == 0;
+}
+
+// The norm of a step whose squares add up to sq[0] + ... + sq[n - 1], and the
+// factor that brings it to at most max_norm: 1, or max_norm / norm, or 0 where
+// the norm is not finite.  The same on every lane; every lane of a wave calls it.
+__device__ __forceinline__ float hl_clip_coef(const double* sq, int32_t n, float max_norm, float* norm) {
+  double s = 0.;
+  if (n <= 64) {  // (uniform: few terms, in order)
+    for (int32_t i = 0; i < n; ++i) s += sq[i];
+  } else {
+    for (int32_t i = threadIdx.x & 63; i < n; i += 64) s += sq[i];
+    s = hl_wave_sum(s);
+  }
+  const double d = sqrt(s);
+  *norm = (float)d;
+  if (!(d <= 1.7976931348623157e308)) return 0.f;
+  return d > (double)max_norm ? (float)((double)max_norm / d) : 1.f;
+}

@@ -42,9 +42,11 @@ struct hl_ws_rec {
   const void* ws;      // NULL: free
   int64_t n, bags;     // the plan's lookups and bags
   int32_t stg;         // its staging rows
-  int part1;           // the first half of the apply ran on it (3: without its spanning segments)
+  int part1;           // the first half of the apply ran on it (3: without its spanning segments), or the
+                       // norm (4: it keeps every group's sum)
   int vec;             // the row vector width that half used (its tile layout depends on it)
   int compact;         // the plan used the layout without the staging-row sums (whole applies only)
+  uint32_t n_hot;      // the hot set's size, which the keys depend on
 };
 struct hl_handle {
   int device;
@@ -105,7 +107,7 @@ static inline void hl_ws_note(hl_handle* h, const void* ws, int kind, int64_t n 
     r = &h->ws_rec[h->ws_next];
     h->ws_next = (h->ws_next + 1) % 4;
   }
-  *r = {ws, n, bags, stg, 0};
+  *r = {ws, n, bags, stg, 0, 0, 0, h->n_hot};
 }
 static inline hl_ws_rec* hl_ws_find(hl_handle* h, const void* ws) {
   for (auto& r : h->ws_rec)
@@ -141,6 +143,14 @@ __device__ __forceinline__ uint32_t hl_fdiv(uint32_t n, uint32_t d, float inv, u
   do {                                                 \
     if (hipGetLastError() != hipSuccess) return HL_ERR_HIP; \
   } while (0)
+
+// The handle's device is the current one (a launch elsewhere could not read the
+// handle's memory).
+static inline hl_status hl_on_device(const struct hl_handle* h) {
+  int d = -1;
+  HL_HIP(hipGetDevice(&d));
+  return d == h->device ? HL_OK : HL_ERR_INVALID_ARG;
+}
 
 __device__ __forceinline__ void hl_flag(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }
 
@@ -195,6 +205,7 @@ __device__ __forceinline__ int32_t hl_hot_slot(const uint64_t* __restrict__ bm,
 #define HL_HDR_DISP 64   // 2 words: dispatch ticket
 #define HL_HDR_GT 72     // 2 words: ticket of the tables' sorts beside the forward
 #define HL_HDR_GBAD 80   // 8 published words (64-bit) of the checks of their bags
+#define HL_HDR_GRAD 96   // 2 words: ticket of a norm's blocks
 #define HL_HDR_GSTAT 128 // 64 published words (64-bit) of theirs
 #define HL_HDR_DSTAT 256 // dispatch's published words (64-bit), to the header's end
 #define HL_DISP_MAX_TILES ((HL_WS_HEADER - 4 * HL_HDR_DSTAT) / 8)

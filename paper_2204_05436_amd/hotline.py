@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # HOTLINE_LIB names another build of the same library (a host-sanitized copy)
 LIB_PATH = os.environ.get("HOTLINE_LIB") or os.path.join(_HERE, "libhotline.so")
 
-HL_F32, HL_BF16 = 0, 1
+HL_F32, HL_BF16, HL_F16 = 0, 1, 2
 STATUS = {0: "ok", 1: "invalid argument", 2: "out of range", 3: "capacity exceeded", 4: "HIP runtime error",
           5: "unsupported", 6: "device error word set"}
 DEVERR = {"OUT_OF_RANGE": 0x1, "BAD_CODE": 0x2, "CAPACITY": 0x4, "BAD_HOTSET": 0x8, "STALL": 0x10,
@@ -41,6 +41,17 @@ class StepIO(C.Structure):
                 ("nonpop_ids", P), ("counts", P), ("cold_ids", P), ("n_cold", P), ("w_host", P), ("w_hot", P),
                 ("staging", P), ("staging_cap", I32), ("out", P), ("workspace", P), ("ws_bytes", SZ),
                 ("write_back", I32), ("step_flags", U32)]
+
+
+class RouteStruct(C.Structure):
+    """hl_route of include/hotline.h, field for field."""
+    _fields_ = [("n_tokens", I64), ("k", I32), ("n_experts", I32), ("capacity", I32), ("align", I32), ("n_rows", I64),
+                ("counts", P), ("offsets", P), ("pos", P), ("order", P)]
+
+
+class GradStruct(C.Structure):
+    """hl_grad of include/hotline.h, field for field."""
+    _fields_ = [("src", P), ("dst", P), ("n", I64), ("dtype", I32)]
 
 
 HL_STEP_UNTIED = 1
@@ -87,6 +98,18 @@ _SIGS = {
     "hl_embbag_bwd_grouping": (C.c_int, [P, I32, I32, I32, I64, P, SZ, P, P, P]),
     "hl_noalloc_scratch_bytes": (SZ, []),
     "hl_embbag_bwd_sgd_noalloc": (C.c_int, [P, P, P, I32, P, P, I32, I32, I64, P, P, I32, P, F32, P]),
+    "hl_route_rows": (I64, [I64, I32, I32, I32, I32]),
+    "hl_route_workspace_bytes": (SZ, [I64, I32, I32]),
+    "hl_route_plan": (C.c_int, [P, P, P, P, SZ, P]),
+    "hl_route_gather": (C.c_int, [P, P, I32, I32, P, I64, P, I64, P]),
+    "hl_route_gather_bwd": (C.c_int, [P, P, I32, I32, P, I64, P, I64, P]),
+    "hl_route_combine": (C.c_int, [P, P, I32, I32, P, I64, P, P, I64, P]),
+    "hl_route_combine_bwd": (C.c_int, [P, P, I32, I32, P, I64, P, I64, P, P, I64, P, P]),
+    "hl_grad_workspace_bytes": (SZ, []),
+    "hl_grad_sq": (C.c_int, [P, P, I32, P, P, SZ, P]),
+    "hl_grad_clip": (C.c_int, [P, P, I32, P, I32, F32, P, P]),
+    "hl_embbag_bwd_norm": (C.c_int, [P, I32, I32, I32, I64, P, P, P, SZ, P]),
+    "hl_embbag_bwd_clip": (C.c_int, [P, P, P, I32, I32, I32, I64, P, I32, F32, F32, P, SZ, P, P]),
     "hl_last_device_error": (C.c_int, [P, C.POINTER(U32)]),
     "hl_debug_ballot_ranks": (C.c_int, [P, I32]),
     "hl_trace_enable": (C.c_int, [P, I32]),
@@ -183,6 +206,12 @@ def _s(stream):
 
 def _nbytes(t):
     return t.numel() * t.element_size()
+
+
+def _check_plain(x, dtype, n, what):
+    """x holds n contiguous elements of dtype (a torch type's name)."""
+    if str(x.dtype) != "torch." + dtype or not x.is_contiguous() or x.numel() < n:
+        raise ValueError(f"{what}: {n} contiguous {dtype} elements wanted, got {x.dtype} {tuple(x.shape)}")
 
 
 class Handle:
@@ -441,6 +470,154 @@ def hl_embbag_bwd_grouping(h, staging_rows, n_samples, bags_per_sample, n_lookup
     _ck("hl_embbag_bwd_grouping", lib().hl_embbag_bwd_grouping(
         h.ptr, int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(ws), _nbytes(ws),
         _p(keys_out), _p(bags_out), _s(stream)))
+
+
+def hl_embbag_bwd_norm(h, staging_rows, n_samples, bags_per_sample, n_lookups, dY, sq, ws, stream=None):
+    """sq: a float64 tensor, its first entry written."""
+    _check_plain(sq, "float64", 1, "sq")
+    _ck("hl_embbag_bwd_norm", lib().hl_embbag_bwd_norm(
+        h.ptr, int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(dY), _p(sq), _p(ws),
+        _nbytes(ws), _s(stream)))
+
+
+def hl_embbag_bwd_clip(h, w_hot, staging, staging_rows, n_samples, bags_per_sample, n_lookups, sq, max_norm, lr, ws,
+                       norm_out=None, stream=None):
+    """sq: float64 tensor of the norm's parts, every entry used."""
+    _check_plain(sq, "float64", 1, "sq")
+    if norm_out is not None:
+        _check_plain(norm_out, "float32", 1, "norm_out")
+    _ck("hl_embbag_bwd_clip", lib().hl_embbag_bwd_clip(
+        h.ptr, _p(w_hot), _p(staging), int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(sq),
+        sq.numel(), float(max_norm), float(lr), _p(ws), _nbytes(ws), _p(norm_out), _s(stream)))
+
+
+# ------------------------------------------------------------------ routing
+def _dt(x):
+    """The hl_dtype of a tensor (bf16 and fp16 by their torch types)."""
+    import torch
+    dt = {torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16}.get(x.dtype)
+    if dt is None:
+        raise TypeError(f"float32, bfloat16 or float16 wanted, got {x.dtype}")
+    return dt
+
+
+def hl_route_rows(n_tokens, k, n_experts, capacity=0, align=1):
+    return int(lib().hl_route_rows(int(n_tokens), int(k), int(n_experts), int(capacity), int(align)))
+
+
+def hl_route_workspace_bytes(n_tokens, k, n_experts):
+    return int(lib().hl_route_workspace_bytes(int(n_tokens), int(k), int(n_experts)))
+
+
+class Route:
+    """A routing plan's sizes and its int32 device arrays (hl_route): counts
+    [n_experts], offsets [n_experts + 1], pos [n_tokens * k] and, if wanted, order
+    [at least hl_route_rows(...)].  n_rows: the rows that order and the buffers of
+    experts' rows hold (None: order's length, or hl_route_rows(...))."""
+
+    def __init__(self, n_tokens, k, n_experts, counts, offsets, pos, order=None, capacity=0, align=1, n_rows=None):
+        _check_plain(counts, "int32", n_experts, "counts")
+        _check_plain(offsets, "int32", n_experts + 1, "offsets")
+        _check_plain(pos, "int32", n_tokens * k, "pos")
+        if n_rows is None:
+            n_rows = hl_route_rows(n_tokens, k, n_experts, capacity, align) if order is None else order.numel()
+        if order is not None:
+            _check_plain(order, "int32", n_rows, "order")
+        self.n_tokens, self.k, self.n_experts, self.n_rows = int(n_tokens), int(k), int(n_experts), int(n_rows)
+        self.counts, self.offsets, self.pos, self.order = counts, offsets, pos, order
+        self.struct = RouteStruct(self.n_tokens, self.k, self.n_experts, int(capacity), int(align), self.n_rows,
+                                  _p(counts), _p(offsets), _p(pos), _p(order))
+
+
+def _rows_arg(x, rows, like, what):
+    """A row buffer's stride: at least `rows` rows like `like`'s, its elements contiguous."""
+    if x.dim() != 2 or x.dtype != like.dtype or x.shape[1:] != like.shape[1:] or x.shape[0] < rows:
+        raise ValueError(f"{what}: {rows} rows like {tuple(like.shape)} {like.dtype} wanted, got {tuple(x.shape)} "
+                         f"{x.dtype}")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{what}: a row's elements must be contiguous")
+    return max(int(x.stride(0)), int(x.shape[1])) if x.shape[0] < 2 else int(x.stride(0))
+
+
+def _weights_arg(w, route, what):
+    if w is not None:
+        _check_plain(w, "float32", route.n_tokens * route.k, what)
+
+
+def hl_route_plan(h, route, experts, ws=None, stream=None):
+    _check_plain(experts, "int32", route.n_tokens * route.k, "experts")
+    _ck("hl_route_plan", lib().hl_route_plan(h.ptr, C.byref(route.struct), _p(experts), _p(ws),
+                                             0 if ws is None else _nbytes(ws), _s(stream)))
+
+
+def hl_route_gather(h, route, x, rows, stream=None):
+    xs, rs = _rows_arg(x, route.n_tokens, x, "x"), _rows_arg(rows, route.n_rows, x, "rows")
+    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, C.byref(route.struct), _dt(x), x.shape[1], _p(x), xs, _p(rows),
+                                                 rs, _s(stream)))
+
+
+def hl_route_gather_bwd(h, route, drows, dx, stream=None):
+    rs, xs = _rows_arg(drows, route.n_rows, drows, "drows"), _rows_arg(dx, route.n_tokens, drows, "dx")
+    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, C.byref(route.struct), _dt(drows), drows.shape[1],
+                                                         _p(drows), rs, _p(dx), xs, _s(stream)))
+
+
+def hl_route_combine(h, route, rows, weights, out, stream=None):
+    rs, os_ = _rows_arg(rows, route.n_rows, rows, "rows"), _rows_arg(out, route.n_tokens, rows, "out")
+    _weights_arg(weights, route, "weights")
+    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, C.byref(route.struct), _dt(rows), rows.shape[1], _p(rows), rs,
+                                                   _p(weights), _p(out), os_, _s(stream)))
+
+
+def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, stream=None):
+    """rows may be None where dweights is."""
+    ds, drs = _rows_arg(dout, route.n_tokens, dout, "dout"), _rows_arg(drows, route.n_rows, dout, "drows")
+    rs = 0 if rows is None else _rows_arg(rows, route.n_rows, dout, "rows")
+    _weights_arg(weights, route, "weights")
+    _weights_arg(dweights, route, "dweights")
+    _ck("hl_route_combine_bwd", lib().hl_route_combine_bwd(
+        h.ptr, C.byref(route.struct), _dt(dout), dout.shape[1], _p(dout), ds, _p(rows), rs, _p(weights), _p(drows), drs,
+        _p(dweights), _s(stream)))
+
+
+# ------------------------------------------------------------------ clipping
+class GradList:
+    """A list of contiguous gradient tensors (float32, bfloat16 or float16) for
+    hl_grad_sq and hl_grad_clip, and where their clipped values go (None: in
+    place).  Holds the tensors; their addresses must not change."""
+
+    def __init__(self, grads, out=None):
+        self.grads, self.out = list(grads), None if out is None else list(out)
+        dst = self.grads if self.out is None else self.out
+        if len(dst) != len(self.grads):
+            raise ValueError(f"{len(self.grads)} gradients, {len(dst)} outputs")
+        self.array = (GradStruct * max(1, len(self.grads)))()
+        for a, g, d in zip(self.array, self.grads, dst):
+            if not g.is_contiguous() or not d.is_contiguous() or d.dtype != g.dtype or d.numel() != g.numel():
+                raise ValueError("gradients and their outputs: contiguous, of the same type and size")
+            a.src, a.dst, a.n, a.dtype = _p(g), _p(d), g.numel(), _dt(g)
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def hl_grad_workspace_bytes():
+    return int(lib().hl_grad_workspace_bytes())
+
+
+def hl_grad_sq(h, grads, sq, ws, stream=None):
+    """grads: a GradList; sq: a float64 tensor, its first entry written."""
+    _check_plain(sq, "float64", 1, "sq")
+    _ck("hl_grad_sq", lib().hl_grad_sq(h.ptr, grads.array, len(grads), _p(sq), _p(ws), _nbytes(ws), _s(stream)))
+
+
+def hl_grad_clip(h, grads, sq, max_norm, norm_out=None, stream=None):
+    """sq: float64 tensor of the norm's parts, every entry used."""
+    _check_plain(sq, "float64", 1, "sq")
+    if norm_out is not None:
+        _check_plain(norm_out, "float32", 1, "norm_out")
+    _ck("hl_grad_clip", lib().hl_grad_clip(h.ptr, grads.array, len(grads), _p(sq), sq.numel(), float(max_norm),
+                                           _p(norm_out), _s(stream)))
 
 
 def hl_debug_ballot_ranks(h, on):
