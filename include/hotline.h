@@ -450,8 +450,8 @@ hl_status hl_route_plan(hl_handle* h, const hl_route* r, const int32_t* experts,
                         hl_stream stream);
 
 /* The row movements.  Rows hold dim elements of dtype (HL_F32, HL_BF16, HL_F16),
- * stride elements apart (stride >= dim), at any address and stride that an
- * element's alignment allows; the handle's tables play no part.  x, out, dout and
+ * stride elements apart (dim <= stride <= 2^31, dim <= 2^20), at any address that
+ * an element's alignment allows; the handle's tables play no part.  x, out, dout and
  * dx are token rows [n_tokens], rows and drows experts' rows [n_rows]; weights and
  * dweights are fp32 [n_tokens*k].  Outputs overlap no input.  Sums are held in
  * fp32 and rounded once, to nearest even; their order is fixed.  An assignment

@@ -695,9 +695,9 @@ bw_reduce2(uint32_t n_tiles, eb_geom g, void* w_hot, void* stg, uint32_t n_hot, 
                                   gc_rows, nullptr);
 }
 
-// The norm's second kernel: the segments that span tiles, and the sum of every
-// block's squares (the first kernel's n1 at nsq, this one's behind them, each block
-// with its share of the first's).
+// The norm's second kernel: the segments that span tiles, and each block's share of
+// the first kernel's n1 sums of squares at nsq; their own sums behind those, added
+// up by the block that finishes last (few blocks: out) or by hl_sum_parts.
 template <int VEC, bool BF>
 __global__ void __launch_bounds__(RB_BLOCK)
 bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const float* __restrict__ tlast,
@@ -710,7 +710,12 @@ bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const fl
   const uint32_t i0 = (uint32_t)((uint64_t)bid * n1 / n2), i1 = (uint32_t)((uint64_t)(bid + 1) * n1 / n2);
   for (uint32_t i = i0 + threadIdx.x; i < i1; i += RB_BLOCK) ss += nsq[i];
   __syncthreads();
-  if (hl_grid_sum(ss, nsq + n1, ticket, n2, err, &total)) *out = total;
+  if (out) {
+    if (hl_grid_sum(ss, nsq + n1, ticket, n2, err, &total)) *out = total;
+    return;
+  }
+  total = hl_block_sum(ss);
+  if (threadIdx.x == 0) nsq[n1 + bid] = total;
 }
 
 // The clipped update from the sums that the norm kept: every position that holds
@@ -1422,10 +1427,12 @@ template <int VEC, bool BF>
 static void launch_norm(const hl_handle* h, uint32_t tiles, hipStream_t s, const uint32_t* sk, const uint32_t* sv,
                         uint32_t n, const float* dY, eb_geom g, bw_ws& ws, uint32_t* ticket, double* sq) {
   const dim3 grid(tiles, g.cchunks), grid2(bw_r2_blocks(tiles, g), g.cchunks);
+  const uint32_t n1 = grid.x * grid.y, n2 = grid2.x * grid2.y;
   HL_KERNEL(h, s, "bw_norm1", (bw_reduce1<VEC, BF, BW_NORM>), grid, dim3(RB_BLOCK), 0, s, sk, sv, n, dY, g, nullptr,
             nullptr, h->n_hot, 0.f, ws.tfirst, ws.tlast, ws.tflag, ws.tkey, ws.gc, ws.gc_rows, ws.bnd, ws.nsq, hl_hook{});
   HL_KERNEL(h, s, "bw_norm2", (bw_norm2<VEC, BF>), grid2, dim3(RB_BLOCK), 0, s, tiles, g, ws.tfirst, ws.tlast, ws.tflag,
-            ws.tkey, ws.gc, ws.nsq, grid.x * grid.y, ticket, sq, h->d_err);
+            ws.tkey, ws.gc, ws.nsq, n1, ticket, n2 <= HL_SUM_TICKETS ? sq : nullptr, h->d_err);
+  if (n2 > HL_SUM_TICKETS) hl_sum_parts(h, ws.nsq + n1, n2, nullptr, sq, s);
 }
 
 extern "C" hl_status hl_embbag_bwd_norm(hl_handle* h, int32_t stg_rows, int32_t n_samples, int32_t bps,

@@ -28,6 +28,15 @@ __device__ __forceinline__ double hl_block_sum(double v) {
 // part[block], and the taker of the last ticket adds them.  True on thread 0 of
 // that block, with the sum in *total.  A header that was not zero-filled, or that
 // overlapping calls share, hands out tickets past n: HL_DEVERR_INTERNAL.
+// The sums are stored and loaded with agent-scope atomics, which bypass the L2s
+// that the XCDs do not share, and a block takes its ticket when its store has
+// completed: no fence, which would write back and invalidate a whole L2 per block.
+// The tickets come one after another, so this is for few blocks (HL_SUM_TICKETS);
+// more leave their sums to a launch of their own (hl_sum_parts).  The norm of 213,000
+// lookups' gradients, 1,200 blocks: with fences 25.9 us, tickets 19.4, and NORM2_US
+// with the launch.
+#define HL_SUM_TICKETS 64
+void hl_sum_parts(const hl_handle* h, const double* part, uint32_t n, const double* run, double* out, hipStream_t s);
 __device__ __forceinline__ bool hl_grid_sum(double v, double* part, uint32_t* ticket, uint32_t n, uint32_t* err,
                                             double* total) {
   __shared__ uint32_t s_last;
@@ -39,7 +48,7 @@ __device__ __forceinline__ bool hl_grid_sum(double v, double* part, uint32_t* ti
   }
   if (threadIdx.x == 0) {
     __hip_atomic_store(part + bid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __threadfence();  // the sum before the ticket
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     uint32_t epoch;
     const uint32_t t = hl_ticket(ticket, n, &epoch);
     if (t >= n) hl_flag(err, HL_DEVERR_INTERNAL);
@@ -47,11 +56,19 @@ __device__ __forceinline__ bool hl_grid_sum(double v, double* part, uint32_t* ti
   }
   __syncthreads();
   if (!s_last) return false;
-  __threadfence();
-  double x = 0.;
-  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x)
-    x += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  *total = hl_block_sum(x);
+  double x[4] = {0., 0., 0., 0.};
+  for (uint32_t i = threadIdx.x; i < n; i += 4 * blockDim.x) {
+    double y[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t j = i + q * blockDim.x;
+      y[q] = __hip_atomic_load(part + min(j, n - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (j >= n) y[q] = 0.;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] += y[q];
+  }
+  *total = hl_block_sum((x[0] + x[1]) + (x[2] + x[3]));
   return threadIdx.x == 0;
 }
 

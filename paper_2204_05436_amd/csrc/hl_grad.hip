@@ -8,49 +8,54 @@
 #include "hl_vec.h"
 
 // The tensors of a launch ride in its arguments (no device table to fill, nothing
-// that a captured graph or a later call could find changed): GR_MAX of them, more
-// in further launches.  Each is cut into chunks of GR_CHUNK bytes, one per step of
-// a block; a block takes consecutive chunks, and finds the tensor of each by two
-// ballots over the tensors' first chunks, which its lanes hold.
-#define GR_MAX 112
+// that a captured graph or a later call could find changed), as many as 4 KB of
+// arguments hold, more in further launches.  Each is cut into chunks of GR_CHUNK
+// bytes, one per step of a block; a block takes consecutive chunks, and finds the
+// tensor of each by ballots over the tensors' first chunks, which its lanes hold.
 #define GR_CHUNK 32768
 #define GR_PARTS (GR_CHUNK / 16 / 256)  // 16-byte parts of a chunk per thread
 #define GR_BLOCKS 2048
 
-struct gr_ent {
-  const void* src;
-  void* dst;
-  int64_t n;
-  uint32_t c0;  // first chunk
-  int32_t dtype;
-};
+template <int MAX, bool DST>
 struct gr_args {
-  gr_ent e[GR_MAX];
+  static constexpr int N = MAX;
+  const void* src[MAX];
+  void* dst[DST ? MAX : 1];
+  int64_t n[MAX];       // elements, shifted left by two, and the type
+  uint32_t c0[MAX];     // first chunk
+  int32_t m;            // tensors
+  uint32_t chunks, per; // chunks in all, and per block
 };
+typedef gr_args<192, false> gr_sq_args;
+typedef gr_args<128, true> gr_clip_args;
 
+template <class A>
 struct gr_find {
-  uint32_t a, b;  // first chunks of tensors lane and lane + 64
-  __device__ __forceinline__ gr_find(const gr_args& g, int m) {
+  uint32_t c[A::N / 64];  // first chunks of tensors lane, lane + 64, ...
+  __device__ __forceinline__ gr_find(const A& g) {
     const int lane = threadIdx.x & 63;
-    a = lane < m ? g.e[lane].c0 : ~0u;
-    b = lane + 64 < m ? g.e[lane + 64].c0 : ~0u;
+#pragma unroll
+    for (int q = 0; q < A::N / 64; ++q) c[q] = lane + 64 * q < g.m ? g.c0[lane + 64 * q] : ~0u;
   }
-  // the last tensor that starts at or before chunk c (an empty one starts where the next does)
-  __device__ __forceinline__ int operator()(uint32_t c) const {
-    return __popcll(__ballot(a <= c)) + __popcll(__ballot(b <= c)) - 1;
+  // the last tensor that starts at or before chunk x (an empty one starts where the next does)
+  __device__ __forceinline__ int operator()(uint32_t x) const {
+    int t = -1;
+#pragma unroll
+    for (int q = 0; q < A::N / 64; ++q) t += __popcll(__ballot(c[q] <= x));
+    return __builtin_amdgcn_readfirstlane(t);
   }
 };
 
 template <class T>
-__device__ __forceinline__ void gr_sum(const gr_ent& e, uint32_t c, double* acc) {
+__device__ __forceinline__ void gr_sum(const void* src, int64_t n, uint32_t c, double* acc) {
   constexpr int N = hl_vec<T>::N;
-  const T* p = (const T*)e.src;
-  const int64_t i0 = (int64_t)(c - e.c0) * (GR_CHUNK / sizeof(T)) + threadIdx.x * N;
+  const T* p = (const T*)src;
+  const int64_t i0 = (int64_t)c * (GR_CHUNK / sizeof(T)) + threadIdx.x * N;
   typename hl_vec<T>::Raw v[GR_PARTS];
 #pragma unroll
   for (int k = 0; k < GR_PARTS; ++k) {
     const int64_t i = i0 + (int64_t)k * 256 * N;
-    v[k] = i < e.n ? hl_vec<T>::load(p + i, e.n - i) : hl_vec<T>::zero();
+    v[k] = i < n ? hl_vec<T>::load(p + i, n - i) : hl_vec<T>::zero();
   }
 #pragma unroll
   for (int k = 0; k < GR_PARTS; ++k)
@@ -62,39 +67,42 @@ __device__ __forceinline__ void gr_sum(const gr_ent& e, uint32_t c, double* acc)
 }
 
 // Squares and sums in 64 bits: an fp32 square overflows from 1.8e19 on.  The
-// blocks' sums are added in block order by the block that finishes last, so the
-// result depends only on the tensors' sizes and values.
+// blocks' sums are added in block order, so the result depends only on the
+// tensors' sizes and values: with few blocks by the one that finishes last
+// (out), otherwise by gr_total.
 __global__ void __launch_bounds__(256)
-gr_sq(gr_args g, int m, uint32_t chunks, uint32_t per, double* part, uint32_t* ticket, double* run, int first,
-      double* out, uint32_t* err) {
-  const gr_find find(g, m);
+gr_sq(gr_sq_args g, double* part, uint32_t* ticket, double* out, uint32_t* err) {
+  const gr_find<gr_sq_args> find(g);
   double acc[4] = {0., 0., 0., 0.};
-  const uint32_t c1 = min(chunks, (blockIdx.x + 1) * per);
-  for (uint32_t c = blockIdx.x * per; c < c1; ++c) {
-    const gr_ent& e = g.e[__builtin_amdgcn_readfirstlane(find(c))];
-    if (e.dtype == HL_F32) gr_sum<float>(e, c, acc);
-    else if (e.dtype == HL_BF16) gr_sum<__bf16>(e, c, acc);
-    else gr_sum<_Float16>(e, c, acc);
+  for (uint32_t c = blockIdx.x; c < g.chunks; c += gridDim.x) {
+    const int t = find(c);
+    const int64_t n = g.n[t];
+    const uint32_t at = c - g.c0[t];
+    if ((n & 3) == HL_F32) gr_sum<float>(g.src[t], n >> 2, at, acc);
+    else if ((n & 3) == HL_BF16) gr_sum<__bf16>(g.src[t], n >> 2, at, acc);
+    else gr_sum<_Float16>(g.src[t], n >> 2, at, acc);
   }
+  const double sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
   double total;
-  if (hl_grid_sum((acc[0] + acc[1]) + (acc[2] + acc[3]), part, ticket, gridDim.x, err, &total)) {
-    if (!first) total += *run;
-    if (out) *out = total;
-    else *run = total;
+  if (out) {
+    if (hl_grid_sum(sum, part, ticket, gridDim.x, err, &total)) *out = total;
+    return;
   }
+  total = hl_block_sum(sum);
+  if (threadIdx.x == 0) part[blockIdx.x] = total;
 }
 
 template <class T>
-__device__ __forceinline__ void gr_scale(const gr_ent& e, uint32_t c, float coef) {
+__device__ __forceinline__ void gr_scale(const void* src, void* dst, int64_t n, uint32_t c, float coef) {
   constexpr int N = hl_vec<T>::N;
-  const T* p = (const T*)e.src;
-  T* q = (T*)e.dst;
-  const int64_t i0 = (int64_t)(c - e.c0) * (GR_CHUNK / sizeof(T)) + threadIdx.x * N;
+  const T* p = (const T*)src;
+  T* q = (T*)dst;
+  const int64_t i0 = (int64_t)c * (GR_CHUNK / sizeof(T)) + threadIdx.x * N;
   typename hl_vec<T>::Raw v[GR_PARTS];
 #pragma unroll
   for (int k = 0; k < GR_PARTS; ++k) {
     const int64_t i = i0 + (int64_t)k * 256 * N;
-    if (i < e.n) v[k] = hl_vec<T>::load(p + i, e.n - i);
+    if (i < n) v[k] = hl_vec<T>::load(p + i, n - i);
   }
 #pragma unroll
   for (int k = 0; k < GR_PARTS; ++k) {
@@ -102,28 +110,34 @@ __device__ __forceinline__ void gr_scale(const gr_ent& e, uint32_t c, float coef
     float o[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) o[j] = coef == 0.f ? 0.f : (float)v[k][j] * coef;
-    if (i < e.n) hl_vec<T>::store(q + i, e.n - i, hl_vec<T>::pack(o));
+    if (i < n) hl_vec<T>::store(q + i, n - i, hl_vec<T>::pack(o));
   }
 }
 
+// (the chunks in descending order: gr_sq read them in ascending order, so the last
+// ones may still be in the memory-side cache)
 __global__ void __launch_bounds__(256)
-gr_clip(gr_args g, int m, uint32_t chunks, uint32_t per, const double* __restrict__ sq, int32_t n_sq, float max_norm,
-        float* norm_out) {
+gr_clip(gr_clip_args g, const double* __restrict__ sq, int32_t n_sq, float max_norm, float* norm_out) {
   float norm;
   const float coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-  const gr_find find(g, m);
-  const uint32_t c1 = min(chunks, (blockIdx.x + 1) * per);
-  for (uint32_t c = blockIdx.x * per; c < c1; ++c) {
-    const gr_ent& e = g.e[__builtin_amdgcn_readfirstlane(find(c))];
-    if (coef == 1.f && e.src == e.dst) continue;
-    if (e.dtype == HL_F32) gr_scale<float>(e, c, coef);
-    else if (e.dtype == HL_BF16) gr_scale<__bf16>(e, c, coef);
-    else gr_scale<_Float16>(e, c, coef);
+  const gr_find<gr_clip_args> find(g);
+  for (uint32_t i = blockIdx.x; i < g.chunks; i += gridDim.x) {
+    const uint32_t c = g.chunks - 1 - i;
+    const int t = find(c);
+    const int64_t n = g.n[t];
+    const uint32_t at = c - g.c0[t];
+    if (coef == 1.f && g.src[t] == g.dst[t]) continue;
+    if ((n & 3) == HL_F32) gr_scale<float>(g.src[t], g.dst[t], n >> 2, at, coef);
+    else if ((n & 3) == HL_BF16) gr_scale<__bf16>(g.src[t], g.dst[t], n >> 2, at, coef);
+    else gr_scale<_Float16>(g.src[t], g.dst[t], n >> 2, at, coef);
   }
 }
 
 // ----------------------------------------------------------------------------- host side
+// The blocks' sums of up to GR_WS_PARTS / GR_BLOCKS launches lie one after another;
+// a list of more launches adds them up in between (run).
+#define GR_WS_PARTS (16 * GR_BLOCKS)
 struct gr_ws {
   uint32_t* ticket;
   double *part, *run;
@@ -133,7 +147,7 @@ static gr_ws gr_carve(void* ws) {
   hl_carver c = hl_carver::after_header(ws, 0);
   gr_ws w;
   w.ticket = c.header() ? c.header() + HL_HDR_GRAD : nullptr;
-  w.part = c.take<double>(GR_BLOCKS);
+  w.part = c.take<double>(GR_WS_PARTS);
   w.run = c.take<double>(1);
   w.bytes = c.off;
   return w;
@@ -160,19 +174,29 @@ static hl_status gr_check(const hl_handle* h, const hl_grad* grads, int32_t n, b
   return hl_on_device(h);
 }
 
-// Fills a launch's arguments with the tensors from grads[i] on; returns their number.
-static int32_t gr_fill(gr_args& a, const hl_grad* grads, int32_t i, int32_t n, uint32_t* chunks) {
-  uint32_t c = 0;
+// Fills a launch's arguments with tensors from grads[i] on; returns their number.
+template <class A>
+static int32_t gr_fill(A& a, const hl_grad* grads, int32_t n) {
+  uint64_t c = 0;
   int32_t m = 0;
-  for (; m < GR_MAX && i + m < n; ++m) {
-    const hl_grad& g = grads[i + m];
+  for (; m < A::N && m < n; ++m) {
+    const hl_grad& g = grads[m];
     const uint64_t need = ((uint64_t)g.n * hl_elem_bytes(g.dtype) + GR_CHUNK - 1) / GR_CHUNK;
     if (m > 0 && c + need > 0x7FFFFFFFull) break;  // (a tensor alone has fewer than 2^28)
-    a.e[m] = {g.src, g.dst, g.n, c, g.dtype};
-    c += (uint32_t)need;
+    a.src[m] = g.src;
+    if (sizeof(a.dst) > sizeof(void*)) a.dst[m] = g.dst;
+    a.n[m] = (g.n << 2) | g.dtype;
+    a.c0[m] = (uint32_t)c;
+    c += need;
   }
-  *chunks = c;
+  a.m = m;
+  a.chunks = (uint32_t)c;
+  a.per = std::max(1u, hl_div_up(c, GR_BLOCKS));
   return m;
+}
+template <class A>
+static uint32_t gr_blocks(const A& a) {
+  return std::max(1u, hl_div_up(a.chunks, a.per));
 }
 
 extern "C" hl_status hl_grad_sq(hl_handle* h, const hl_grad* grads, int32_t n_grads, double* sq, void* workspace,
@@ -184,21 +208,30 @@ extern "C" hl_status hl_grad_sq(hl_handle* h, const hl_grad* grads, int32_t n_gr
   hl_ws_note(h, workspace, HL_WSK_OTHER);
   const gr_ws w = gr_carve(workspace);
   hipStream_t s = (hipStream_t)stream;
-  gr_args a;
-  int32_t i = 0;
-  do {
-    uint32_t chunks = 0;
-    const int32_t m = gr_fill(a, grads, i, n_grads, &chunks);
-    const uint32_t per = std::max(1u, hl_div_up(chunks, GR_BLOCKS));
-    const uint32_t blocks = std::max(1u, hl_div_up(chunks, per));
-    HL_KERNEL(h, s, "gr_sq", gr_sq, dim3(blocks), dim3(256), 0, s, a, m, chunks, per, w.part, w.ticket, w.run,
-              (int)(i == 0), i + m >= n_grads ? sq : nullptr, h->d_err);
-    i += m;
-  } while (i < n_grads);
+  gr_sq_args a;
+  uint32_t parts = 0;
+  bool run = false;
+  for (int32_t i = 0;;) {
+    i += gr_fill(a, grads + i, n_grads - i);
+    const uint32_t blocks = gr_blocks(a);
+    const bool last = i >= n_grads;
+    const bool alone = last && !parts && !run && blocks <= HL_SUM_TICKETS;
+    HL_KERNEL(h, s, "gr_sq", gr_sq, dim3(blocks), dim3(256), 0, s, a, w.part + parts, w.ticket, alone ? sq : nullptr,
+              h->d_err);
+    if (alone) break;
+    parts += blocks;
+    if (last || parts > GR_WS_PARTS - GR_BLOCKS) {
+      hl_sum_parts(h, w.part, parts, run ? w.run : nullptr, last ? sq : w.run, s);
+      parts = 0;
+      run = true;
+    }
+    if (last) break;
+  }
   HL_LAUNCHED();
   return HL_OK;
 }
 
+// The launches in descending order too (gr_clip).
 extern "C" hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int32_t n_grads, const double* sq,
                                   int32_t n_sq, float max_norm, float* norm_out, hl_stream stream) {
   hl_status st = gr_check(h, grads, n_grads, true);
@@ -206,17 +239,37 @@ extern "C" hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int3
   if (!sq || (uintptr_t)sq % 8 != 0 || n_sq < 1 || !(max_norm >= 0.f) || (uintptr_t)norm_out % 4 != 0)
     return HL_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
-  gr_args a;
-  int32_t i = 0;
-  do {
-    uint32_t chunks = 0;
-    const int32_t m = gr_fill(a, grads, i, n_grads, &chunks);
-    const uint32_t per = std::max(1u, hl_div_up(chunks, GR_BLOCKS));
-    const uint32_t blocks = std::max(1u, hl_div_up(chunks, per));
-    HL_KERNEL(h, s, "gr_clip", gr_clip, dim3(blocks), dim3(256), 0, s, a, m, chunks, per, sq, n_sq, max_norm,
-              i == 0 ? norm_out : nullptr);
-    i += m;
-  } while (i < n_grads);
+  gr_clip_args a;
+  for (int32_t end = n_grads;;) {
+    const int32_t from = std::max(0, end - gr_clip_args::N);
+    int32_t i = from;
+    do {  // (once, but for tensors of 2^31 chunks together)
+      i += gr_fill(a, grads + i, end - i);
+      HL_KERNEL(h, s, "gr_clip", gr_clip, dim3(gr_blocks(a)), dim3(256), 0, s, a, sq, n_sq, max_norm,
+                i >= n_grads ? norm_out : nullptr);
+    } while (i < end);
+    end = from;
+    if (end == 0) break;
+  }
   HL_LAUNCHED();
   return HL_OK;
+}
+
+// ----------------------------------------------------------------------------- parts
+__global__ void __launch_bounds__(1024)
+gr_total(const double* __restrict__ part, uint32_t n, const double* run, double* out) {
+  double x[4] = {0., 0., 0., 0.};
+  for (uint32_t i = threadIdx.x; i < n; i += 4096) {
+    double y[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = i + q * 1024 < n ? part[i + q * 1024] : 0.;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] += y[q];
+  }
+  const double t = hl_block_sum((x[0] + x[1]) + (x[2] + x[3]));
+  if (threadIdx.x == 0) *out = run ? *run + t : t;
+}
+
+void hl_sum_parts(const hl_handle* h, const double* part, uint32_t n, const double* run, double* out, hipStream_t s) {
+  HL_KERNEL(h, s, "gr_total", gr_total, dim3(1), dim3(1024), 0, s, part, n, run, out);
 }

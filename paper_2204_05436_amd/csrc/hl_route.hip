@@ -18,6 +18,7 @@
 #define RT_THREADS 1024
 #define RT_WAVES (RT_THREADS / 64)
 #define RT_MAX_EXPERTS 1024
+#define RT_MAX_DIM (1 << 20)
 #define RT_DIRECT 256
 
 struct rt_shape {
@@ -119,6 +120,18 @@ rt_place(const int32_t* __restrict__ experts, rt_shape sh, const uint32_t* __res
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const uint32_t tile = blockIdx.x;
   if (tid < sh.E) s_prev[tid] = s_tot[tid] = 0;
+  // the tiles' counts, loaded beside the ids: every thread adds up some tiles of one expert
+  uint32_t prev = 0, tot = 0;
+  const int he = tid & ((1 << sh.bits) - 1);
+  if (mode == 1 && he < sh.E) {
+    const uint32_t segs = RT_THREADS >> sh.bits;
+#pragma unroll 8
+    for (uint32_t t = (uint32_t)tid >> sh.bits; t < tiles; t += segs) {
+      const uint32_t c = hist[(size_t)t * sh.E + he];
+      tot += c;
+      if (t < tile) prev += c;
+    }
+  }
   int32_t ex[ITEMS];
   uint32_t rk[ITEMS];
   rt_count<ITEMS>(experts, sh, tile, s_cnt, ex, rk, err);
@@ -133,20 +146,9 @@ rt_place(const int32_t* __restrict__ experts, rt_shape sh, const uint32_t* __res
       mine += c;
     }
   }
-  if (mode == 1) {  // every thread adds up some tiles of one expert
-    const int e = tid & ((1 << sh.bits) - 1);
-    const uint32_t seg = (uint32_t)tid >> sh.bits, segs = RT_THREADS >> sh.bits;
-    uint32_t prev = 0, tot = 0;
-    if (e < sh.E) {
-#pragma unroll 8
-      for (uint32_t t = seg; t < tiles; t += segs) {
-        const uint32_t c = hist[(size_t)t * sh.E + e];
-        tot += c;
-        if (t < tile) prev += c;
-      }
-      if (tot) atomicAdd(&s_tot[e], tot);
-      if (prev) atomicAdd(&s_prev[e], prev);
-    }
+  if (mode == 1) {
+    if (tot) atomicAdd(&s_tot[he], tot);
+    if (prev) atomicAdd(&s_prev[he], prev);
   } else if (tid < sh.E) {
     s_prev[tid] = mode == 2 ? hist[(size_t)tile * sh.E + tid] : 0u;
     s_tot[tid] = mode == 2 ? hist[(size_t)tiles * sh.E + tid] : mine;
@@ -213,26 +215,43 @@ static uint32_t rt_tile_count(int64_t n) {
 }
 
 // ----------------------------------------------------------------------------- row movements
-// A row is covered by G lanes of 16 bytes each, G the power of two that the row's
-// 16-byte parts need, at most 64: a wave holds 64 / G tokens, or 64 parts of one,
-// the row's further parts over blockIdx.y.
+// A token's row is covered by 16-byte parts, one per lane: 2^lg lanes take a
+// token's chunk of that many parts, so a block of 256 holds several short rows or
+// 256 parts (4 KB) of one, whose further chunks are the next blocks'.  Neighbouring
+// blocks thus read and write the same rows at the same time; with a wave per 1 KB
+// and the parts over blockIdx.y the rows' pieces came far apart in time, and
+// dispatch-like gathers ran at 4 TB/s and sums of rows at 4.4.
+// UNI: a wave's lanes all hold the same token (lg >= 6), whose rows' addresses are
+// then scalar.  KB: assignments of a token whose rows are in flight together.
 struct rt_geom {
-  int32_t dim, k, lg;  // lg: log2 G
+  int32_t dim, k, lg, chunks;  // lg: log2 of the lanes of a chunk; chunks per row
   int64_t n_tokens, rows;
 };
 
-#define RT_KB 8  // assignments of a token whose rows are in flight together
-
-// The part of a row that this lane holds: token t, column col, n elements left
-// from there (0: none).
-template <class T>
-__device__ __forceinline__ void rt_part(const rt_geom& g, int64_t* t, int64_t* col, int64_t* n) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  *t = (((int64_t)blockIdx.x * 4 + w) << (6 - g.lg)) + (lane >> g.lg);
-  *col = ((int64_t)blockIdx.y * 64 + (lane & ((1 << g.lg) - 1))) * hl_vec<T>::N;
-  *n = *t < g.n_tokens ? g.dim - *col : 0;
+// This lane's token and column; false: none.
+template <class T, bool UNI>
+__device__ __forceinline__ bool rt_part(const rt_geom& g, uint32_t* t, int32_t* col) {
+  uint32_t u, l;
+  if (UNI) {
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    u = blockIdx.x * (256u >> g.lg) + (w >> (g.lg - 6));
+    l = ((w & ((1u << (g.lg - 6)) - 1)) << 6) + (threadIdx.x & 63);
+  } else {
+    u = blockIdx.x * (256u >> g.lg) + (threadIdx.x >> g.lg);
+    l = threadIdx.x & ((1u << g.lg) - 1);
+  }
+  uint32_t c = 0;
+  *t = u;
+  if (g.chunks > 1) {
+    *t = u / (uint32_t)g.chunks;
+    c = u - *t * (uint32_t)g.chunks;
+  }
+  *col = (int32_t)(((c << g.lg) + l) * hl_vec<T>::N);
+  return *t < g.n_tokens && *col < g.dim;
 }
+template <bool UNI>
 __device__ __forceinline__ int32_t rt_row(int32_t p, int64_t rows, uint32_t* err) {
+  if (UNI) p = __builtin_amdgcn_readfirstlane(p);
   if (p == -1) return -1;
   if (p < 0 || p >= rows) {
     hl_flag(err, HL_DEVERR_BAD_CODE);
@@ -240,21 +259,19 @@ __device__ __forceinline__ int32_t rt_row(int32_t p, int64_t rows, uint32_t* err
   }
   return p;
 }
-// The padding rows of expert e's block, set to zero (column part blockIdx.y).
+// The padding rows of expert e's block, set to zero.
 template <class T>
 __device__ __forceinline__ void rt_pad(int e, const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
                                        const rt_geom& g, T* __restrict__ out, int64_t stride) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  constexpr int N = hl_vec<T>::N;
   const int64_t end = min((int64_t)offsets[e + 1], g.rows);
-  const int64_t col = ((int64_t)blockIdx.y * 64 + (lane & ((1 << g.lg) - 1))) * hl_vec<T>::N;
-  const int64_t n = g.dim - col;
-  if (n <= 0) return;
-  for (int64_t r = (int64_t)offsets[e] + counts[e] + (w << (6 - g.lg)) + (lane >> g.lg); r < end;
-       r += 4 << (6 - g.lg))
-    if (r >= 0) hl_vec<T>::store(out + r * stride + col, n, hl_vec<T>::zero());
+  const int lg = min(g.lg, 8);
+  for (int64_t r = (int64_t)offsets[e] + counts[e] + (threadIdx.x >> lg); r < end; r += 256 >> lg)
+    for (int64_t col = (int64_t)(threadIdx.x & ((1 << lg) - 1)) * N; col < g.dim; col += (int64_t)N << lg)
+      if (r >= 0) hl_vec<T>::store(out + r * stride + col, g.dim - col, hl_vec<T>::zero());
 }
 
-template <class T>
+template <class T, bool UNI, int KB>
 __global__ void __launch_bounds__(256)
 rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int32_t* __restrict__ counts,
           const int32_t* __restrict__ offsets, const T* __restrict__ x, int64_t xs, T* __restrict__ out, int64_t os,
@@ -263,56 +280,68 @@ rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int
     rt_pad<T>(blockIdx.x - blocks, counts, offsets, g, out, os);
     return;
   }
-  int64_t t, col, n;
-  rt_part<T>(g, &t, &col, &n);
-  if (n <= 0) return;
+  uint32_t t;
+  int32_t col;
+  if (!rt_part<T, UNI>(g, &t, &col)) return;
+  const int64_t n = g.dim - col;
   const typename hl_vec<T>::Raw v = hl_vec<T>::load(x + t * xs + col, n);
-  for (int j = 0; j < g.k; ++j) {
-    const int32_t p = rt_row(pos[t * g.k + j], g.rows, err);
-    if (p >= 0) hl_vec<T>::store(out + (int64_t)p * os + col, n, v);
+  const int32_t* pt = pos + (int64_t)t * g.k;
+  for (int j0 = 0; j0 < g.k; j0 += KB) {
+    int32_t p[KB];
+#pragma unroll
+    for (int j = 0; j < KB; ++j) p[j] = j0 + j < g.k ? pt[j0 + j] : -1;
+#pragma unroll
+    for (int j = 0; j < KB; ++j) {
+      p[j] = rt_row<UNI>(p[j], g.rows, err);
+      if (p[j] >= 0) hl_vec<T>::store(out + (int64_t)p[j] * os + col, n, v);
+    }
   }
 }
 
-template <class T, bool W>
+template <class T, bool UNI, int KB, bool W>
 __global__ void __launch_bounds__(256)
 rt_combine(rt_geom g, const int32_t* __restrict__ pos, const T* __restrict__ rows, int64_t rs,
            const float* __restrict__ weights, T* __restrict__ out, int64_t os, uint32_t* err) {
   typedef typename hl_vec<T>::Raw Raw;
   constexpr int N = hl_vec<T>::N;
-  int64_t t, col, n;
-  rt_part<T>(g, &t, &col, &n);
-  if (n <= 0) return;
+  uint32_t t;
+  int32_t col;
+  if (!rt_part<T, UNI>(g, &t, &col)) return;
+  const int64_t n = g.dim - col;
+  const int32_t* pt = pos + (int64_t)t * g.k;
+  const float* wt = W ? weights + (int64_t)t * g.k : nullptr;
   float acc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0.f;
-  for (int j0 = 0; j0 < g.k; j0 += RT_KB) {
-    int32_t p[RT_KB];
-    float wt[RT_KB];
-    Raw v[RT_KB];
+  for (int j0 = 0; j0 < g.k; j0 += KB) {
+    int32_t p[KB];
+    float w[KB];
+    Raw v[KB];
 #pragma unroll
-    for (int j = 0; j < RT_KB; ++j) {
-      p[j] = j0 + j < g.k ? pos[t * g.k + j0 + j] : -1;
-      wt[j] = W && j0 + j < g.k ? weights[t * g.k + j0 + j] : 1.f;
+    for (int j = 0; j < KB; ++j) {
+      p[j] = j0 + j < g.k ? pt[j0 + j] : -1;
+      w[j] = W && j0 + j < g.k ? wt[j0 + j] : 1.f;
     }
 #pragma unroll
-    for (int j = 0; j < RT_KB; ++j) {
-      p[j] = rt_row(p[j], g.rows, err);
+    for (int j = 0; j < KB; ++j) {
+      p[j] = rt_row<UNI>(p[j], g.rows, err);
       if (p[j] >= 0) v[j] = hl_vec<T>::load(rows + (int64_t)p[j] * rs + col, n);
     }
 #pragma unroll
-    for (int j = 0; j < RT_KB; ++j)
+    for (int j = 0; j < KB; ++j)
       if (p[j] >= 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = W ? fmaf(wt[j], (float)v[j][i], acc[i]) : acc[i] + (float)v[j][i];
+        for (int i = 0; i < N; ++i) acc[i] = W ? fmaf(w[j], (float)v[j][i], acc[i]) : acc[i] + (float)v[j][i];
       }
   }
   hl_vec<T>::store(out + t * os + col, n, hl_vec<T>::pack(acc));
 }
 
 // The gradients of the weighted sum: an assignment's row of drows is w times the
-// token's gradient, its weight's gradient their dot product.  Groups of G lanes
-// take a token (lg < 6), or a whole block does.
-template <class T>
+// token's gradient, its weight's gradient their dot product.  The lanes of a
+// chunk take all of the token's chunks in turn, and add their dot products up at
+// the end.
+template <class T, bool UNI, int KB>
 __global__ void __launch_bounds__(256)
 rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int32_t* __restrict__ counts,
                const int32_t* __restrict__ offsets, const T* __restrict__ dout, int64_t ds,
@@ -320,43 +349,42 @@ rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, cons
                int64_t drs, float* __restrict__ dweights, uint32_t* err) {
   typedef typename hl_vec<T>::Raw Raw;
   constexpr int N = hl_vec<T>::N;
-  __shared__ float s_dot[4][RT_KB];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const bool whole = g.lg == 6;
+  __shared__ float s_dot[4][KB];
   if (blockIdx.x >= blocks) {
-    // (every part of a padding row in this block)
-    const int e = blockIdx.x - blocks;
-    const int64_t end = min((int64_t)offsets[e + 1], g.rows), first = (int64_t)offsets[e] + counts[e];
-    if (first < 0) return;
-    for (int64_t r = first + w; r < end; r += 4)
-      for (int64_t col = (int64_t)lane * N; col < g.dim; col += 64 * N)
-        hl_vec<T>::store(drows + r * drs + col, g.dim - col, hl_vec<T>::zero());
+    rt_pad<T>(blockIdx.x - blocks, counts, offsets, g, drows, drs);
     return;
   }
-  const int64_t t = whole ? (int64_t)blockIdx.x : (((int64_t)blockIdx.x * 4 + w) << (6 - g.lg)) + (lane >> g.lg);
-  const int64_t c0 = (int64_t)(whole ? threadIdx.x : (lane & ((1 << g.lg) - 1))) * N;
-  const int64_t step = (int64_t)(whole ? 256 : (1 << g.lg)) * N;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t t;
+  int32_t c0;
+  rt_geom g1 = g;
+  g1.chunks = 1;
+  rt_part<T, UNI>(g1, &t, &c0);
   const bool in = t < g.n_tokens;
-  for (int j0 = 0; j0 < g.k; j0 += RT_KB) {
-    int32_t p[RT_KB];
-    float wt[RT_KB], dot[RT_KB];
+  const int32_t* pt = pos + (int64_t)t * g.k;
+  for (int j0 = 0; j0 < g.k; j0 += KB) {
+    int32_t p[KB];
+    float wt[KB], dot[KB];
 #pragma unroll
-    for (int j = 0; j < RT_KB; ++j) {
-      p[j] = in && j0 + j < g.k ? rt_row(pos[t * g.k + j0 + j], g.rows, err) : -1;
-      wt[j] = weights && p[j] >= 0 ? weights[t * g.k + j0 + j] : 1.f;
+    for (int j = 0; j < KB; ++j) {
+      const bool has = in && j0 + j < g.k;
+      p[j] = has ? pt[j0 + j] : -1;
+      wt[j] = has && weights ? weights[(int64_t)t * g.k + j0 + j] : 1.f;
       dot[j] = 0.f;
     }
+#pragma unroll
+    for (int j = 0; j < KB; ++j) p[j] = rt_row<UNI>(p[j], g.rows, err);
     if (in)
-      for (int64_t col = c0; col < g.dim; col += step) {
+      for (int32_t col = c0; col < g.dim; col += N << g.lg) {
         const int64_t n = g.dim - col;
         const Raw d = hl_vec<T>::load(dout + t * ds + col, n);
-        Raw v[RT_KB];
+        Raw v[KB];
         if (dweights)
 #pragma unroll
-          for (int j = 0; j < RT_KB; ++j)
+          for (int j = 0; j < KB; ++j)
             if (p[j] >= 0) v[j] = hl_vec<T>::load(rows + (int64_t)p[j] * rs + col, n);
 #pragma unroll
-        for (int j = 0; j < RT_KB; ++j)
+        for (int j = 0; j < KB; ++j)
           if (p[j] >= 0) {
             float o[N];
 #pragma unroll
@@ -368,23 +396,26 @@ rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, cons
           }
       }
     if (!dweights) continue;
-    for (int o = 1; o < (1 << g.lg); o <<= 1)
+    const int lg = UNI ? 6 : g.lg;
+    for (int o = 1; o < (1 << lg); o <<= 1)
 #pragma unroll
-      for (int j = 0; j < RT_KB; ++j) dot[j] += __shfl_xor(dot[j], o);
-    if (whole) {
+      for (int j = 0; j < KB; ++j) dot[j] += __shfl_xor(dot[j], o);
+    if (UNI && g.lg > 6) {  // a token's waves, in order
       if (lane == 0)
 #pragma unroll
-        for (int j = 0; j < RT_KB; ++j) s_dot[w][j] = dot[j];
+        for (int j = 0; j < KB; ++j) s_dot[w][j] = dot[j];
       __syncthreads();
-      if (threadIdx.x < RT_KB && j0 + (int)threadIdx.x < g.k) {
-        const int j = threadIdx.x;
-        dweights[t * g.k + j0 + j] = (s_dot[0][j] + s_dot[1][j]) + (s_dot[2][j] + s_dot[3][j]);
+      const int wpt = 1 << (g.lg - 6);
+      if (in && (w & (wpt - 1)) == 0 && lane < KB && j0 + lane < g.k) {
+        float s = 0.f;
+        for (int q = 0; q < wpt; ++q) s += s_dot[w + q][lane];
+        dweights[(int64_t)t * g.k + j0 + lane] = s;
       }
       __syncthreads();
-    } else if (in && (lane & ((1 << g.lg) - 1)) == 0) {
+    } else if (in && (lane & ((1 << lg) - 1)) == 0) {
 #pragma unroll
-      for (int j = 0; j < RT_KB; ++j)
-        if (j0 + j < g.k) dweights[t * g.k + j0 + j] = dot[j];
+      for (int j = 0; j < KB; ++j)
+        if (j0 + j < g.k) dweights[(int64_t)t * g.k + j0 + j] = dot[j];
     }
   }
 }
@@ -425,6 +456,7 @@ static hl_status rt_check_rows(const hl_handle* h, const hl_route* r, int32_t dt
   if (st != HL_OK) return st;
   const size_t es = hl_elem_bytes(dtype);
   if (!es || dim < 1) return HL_ERR_INVALID_ARG;
+  if (dim > RT_MAX_DIM) return HL_ERR_UNSUPPORTED;
   if (r->n_tokens == 0) return HL_OK;
   st = rt_rows_ok(a, as, dim, es);
   return st != HL_OK ? st : rt_rows_ok(b, bs, dim, es);
@@ -434,14 +466,23 @@ template <class T>
 static rt_geom rt_make_geom(const hl_route* r, int32_t dim) {
   const int parts = (dim + hl_vec<T>::N - 1) / hl_vec<T>::N;
   int lg = 0;
-  while (lg < 6 && (1 << lg) < parts) ++lg;
-  return {dim, r->k, lg, r->n_tokens, r->n_rows};
+  while (lg < 8 && (1 << lg) < parts) ++lg;
+  return {dim, r->k, lg, (parts + (1 << lg) - 1) >> lg, r->n_tokens, r->n_rows};
 }
-template <class T>
-static dim3 rt_grid(const rt_geom& g) {
-  const int parts = (g.dim + hl_vec<T>::N - 1) / hl_vec<T>::N;
-  return dim3(hl_div_up(g.n_tokens, 4ull << (6 - g.lg)), hl_div_up(parts, 64));
-}
+// KERNEL<T, UNI, KB ...>: the fewest rows in flight that hold a token's, so that no
+// registers are kept for rows it does not have
+#define RT_FORM(g, LAUNCH)                                         \
+  do {                                                             \
+    if ((g).lg >= 6) {                                             \
+      if ((g).k <= 2) LAUNCH(true, 2);                             \
+      else if ((g).k <= 4) LAUNCH(true, 4);                        \
+      else LAUNCH(true, 8);                                        \
+    } else {                                                       \
+      if ((g).k <= 2) LAUNCH(false, 2);                            \
+      else if ((g).k <= 4) LAUNCH(false, 4);                       \
+      else LAUNCH(false, 8);                                       \
+    }                                                              \
+  } while (0)
 
 extern "C" hl_status hl_route_plan(hl_handle* h, const hl_route* r, const int32_t* experts, void* workspace,
                                    size_t ws_bytes, hl_stream stream) {
@@ -481,11 +522,13 @@ template <class T>
 static void launch_gather(const hl_handle* h, const hl_route* r, int32_t dim, const void* x, int64_t xs, void* out,
                           int64_t os, hipStream_t s) {
   const rt_geom g = rt_make_geom<T>(r, dim);
-  dim3 grid = rt_grid<T>(g);
-  const uint32_t blocks = grid.x;
-  if (r->align > 1) grid.x += (uint32_t)r->n_experts;
-  HL_KERNEL(h, s, "rt_gather", (rt_gather<T>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts, r->offsets,
-            (const T*)x, xs, (T*)out, os, h->d_err);
+  const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg);
+  const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
+#define GATHER(U, K)                                                                                                \
+  HL_KERNEL(h, s, "rt_gather", (rt_gather<T, U, K>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts, r->offsets, \
+            (const T*)x, xs, (T*)out, os, h->d_err)
+  RT_FORM(g, GATHER);
+#undef GATHER
 }
 
 extern "C" hl_status hl_route_gather(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim, const void* x,
@@ -501,12 +544,18 @@ template <class T>
 static void launch_combine(const hl_handle* h, const hl_route* r, int32_t dim, const void* rows, int64_t rs,
                            const float* weights, void* out, int64_t os, hipStream_t s) {
   const rt_geom g = rt_make_geom<T>(r, dim);
-  if (weights)
-    HL_KERNEL(h, s, "rt_combine", (rt_combine<T, true>), rt_grid<T>(g), dim3(256), 0, s, g, r->pos, (const T*)rows, rs,
-              weights, (T*)out, os, h->d_err);
-  else
-    HL_KERNEL(h, s, "rt_combine", (rt_combine<T, false>), rt_grid<T>(g), dim3(256), 0, s, g, r->pos, (const T*)rows,
-              rs, weights, (T*)out, os, h->d_err);
+  const dim3 grid(hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg));
+#define COMBINE(U, K)                                                                                               \
+  do {                                                                                                              \
+    if (weights)                                                                                                    \
+      HL_KERNEL(h, s, "rt_combine", (rt_combine<T, U, K, true>), grid, dim3(256), 0, s, g, r->pos, (const T*)rows,  \
+                rs, weights, (T*)out, os, h->d_err);                                                                \
+    else                                                                                                            \
+      HL_KERNEL(h, s, "rt_combine", (rt_combine<T, U, K, false>), grid, dim3(256), 0, s, g, r->pos, (const T*)rows, \
+                rs, weights, (T*)out, os, h->d_err);                                                                \
+  } while (0)
+  RT_FORM(g, COMBINE);
+#undef COMBINE
 }
 
 extern "C" hl_status hl_route_combine(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim,
@@ -531,10 +580,13 @@ static void launch_combine_bwd(const hl_handle* h, const hl_route* r, int32_t di
                                const void* rows, int64_t rs, const float* weights, void* drows, int64_t drs,
                                float* dweights, hipStream_t s) {
   const rt_geom g = rt_make_geom<T>(r, dim);
-  const uint32_t blocks = g.lg == 6 ? (uint32_t)g.n_tokens : hl_div_up(g.n_tokens, 4ull << (6 - g.lg));
-  HL_KERNEL(h, s, "rt_combine_bwd", (rt_combine_bwd<T>), dim3(blocks + (r->align > 1 ? r->n_experts : 0)), dim3(256), 0,
-            s, g, blocks, r->pos, r->counts, r->offsets, (const T*)dout, ds, (const T*)rows, rs, weights, (T*)drows,
-            drs, dweights, h->d_err);
+  const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens, 256 >> g.lg);
+  const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
+#define COMBINE_BWD(U, K)                                                                                            \
+  HL_KERNEL(h, s, "rt_combine_bwd", (rt_combine_bwd<T, U, K>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts,  \
+            r->offsets, (const T*)dout, ds, (const T*)rows, rs, weights, (T*)drows, drs, dweights, h->d_err)
+  RT_FORM(g, COMBINE_BWD);
+#undef COMBINE_BWD
 }
 
 extern "C" hl_status hl_route_combine_bwd(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim,

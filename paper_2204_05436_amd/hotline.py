@@ -195,10 +195,21 @@ def _p(x):
     return x.data_ptr()
 
 
+_raw_stream = None  # the current stream's handle, without a Stream object where torch has a call for that
+
+
+def _current_stream():
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+        _raw_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+    return _raw_stream()
+
+
 def _s(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -492,10 +503,19 @@ def hl_embbag_bwd_clip(h, w_hot, staging, staging_rows, n_samples, bags_per_samp
 
 
 # ------------------------------------------------------------------ routing
+_types = {}  # torch type -> hl_dtype
+
+
+def _torch_types():
+    if not _types:
+        import torch
+        _types.update({torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16})
+    return _types
+
+
 def _dt(x):
     """The hl_dtype of a tensor (bf16 and fp16 by their torch types)."""
-    import torch
-    dt = {torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16}.get(x.dtype)
+    dt = _torch_types().get(x.dtype)
     if dt is None:
         raise TypeError(f"float32, bfloat16 or float16 wanted, got {x.dtype}")
     return dt
@@ -527,16 +547,16 @@ class Route:
         self.counts, self.offsets, self.pos, self.order = counts, offsets, pos, order
         self.struct = RouteStruct(self.n_tokens, self.k, self.n_experts, int(capacity), int(align), self.n_rows,
                                   _p(counts), _p(offsets), _p(pos), _p(order))
+        self.ref = C.byref(self.struct)
 
 
-def _rows_arg(x, rows, like, what):
-    """A row buffer's stride: at least `rows` rows like `like`'s, its elements contiguous."""
-    if x.dim() != 2 or x.dtype != like.dtype or x.shape[1:] != like.shape[1:] or x.shape[0] < rows:
-        raise ValueError(f"{what}: {rows} rows like {tuple(like.shape)} {like.dtype} wanted, got {tuple(x.shape)} "
-                         f"{x.dtype}")
-    if x.shape[1] > 1 and x.stride(1) != 1:
-        raise ValueError(f"{what}: a row's elements must be contiguous")
-    return max(int(x.stride(0)), int(x.shape[1])) if x.shape[0] < 2 else int(x.stride(0))
+def _rows_arg(x, rows, dtype, dim, what):
+    """The stride of a row buffer: at least `rows` rows of dim contiguous elements of dtype."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or x.dtype != dtype or shape[1] != dim or shape[0] < rows or (dim > 1 and stride[1] != 1):
+        raise ValueError(f"{what}: {rows} rows of {dim} contiguous {dtype} elements wanted, got {tuple(shape)} {x.dtype} "
+                         f"with strides {stride}")
+    return stride[0] if shape[0] > 1 else max(stride[0], dim)
 
 
 def _weights_arg(w, route, what):
@@ -546,38 +566,40 @@ def _weights_arg(w, route, what):
 
 def hl_route_plan(h, route, experts, ws=None, stream=None):
     _check_plain(experts, "int32", route.n_tokens * route.k, "experts")
-    _ck("hl_route_plan", lib().hl_route_plan(h.ptr, C.byref(route.struct), _p(experts), _p(ws),
-                                             0 if ws is None else _nbytes(ws), _s(stream)))
+    _ck("hl_route_plan", lib().hl_route_plan(h.ptr, route.ref, _p(experts), _p(ws), 0 if ws is None else _nbytes(ws),
+                                             _s(stream)))
 
 
 def hl_route_gather(h, route, x, rows, stream=None):
-    xs, rs = _rows_arg(x, route.n_tokens, x, "x"), _rows_arg(rows, route.n_rows, x, "rows")
-    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, C.byref(route.struct), _dt(x), x.shape[1], _p(x), xs, _p(rows),
-                                                 rs, _s(stream)))
+    dt, d = x.dtype, x.shape[-1]
+    xs, rs = _rows_arg(x, route.n_tokens, dt, d, "x"), _rows_arg(rows, route.n_rows, dt, d, "rows")
+    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, route.ref, _dt(x), d, _p(x), xs, _p(rows), rs, _s(stream)))
 
 
 def hl_route_gather_bwd(h, route, drows, dx, stream=None):
-    rs, xs = _rows_arg(drows, route.n_rows, drows, "drows"), _rows_arg(dx, route.n_tokens, drows, "dx")
-    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, C.byref(route.struct), _dt(drows), drows.shape[1],
-                                                         _p(drows), rs, _p(dx), xs, _s(stream)))
+    dt, d = drows.dtype, drows.shape[-1]
+    rs, xs = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx")
+    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, _dt(drows), d, _p(drows), rs, _p(dx), xs,
+                                                         _s(stream)))
 
 
 def hl_route_combine(h, route, rows, weights, out, stream=None):
-    rs, os_ = _rows_arg(rows, route.n_rows, rows, "rows"), _rows_arg(out, route.n_tokens, rows, "out")
+    dt, d = rows.dtype, rows.shape[-1]
+    rs, os_ = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out")
     _weights_arg(weights, route, "weights")
-    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, C.byref(route.struct), _dt(rows), rows.shape[1], _p(rows), rs,
-                                                   _p(weights), _p(out), os_, _s(stream)))
+    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, route.ref, _dt(rows), d, _p(rows), rs, _p(weights), _p(out), os_,
+                                                   _s(stream)))
 
 
 def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, stream=None):
     """rows may be None where dweights is."""
-    ds, drs = _rows_arg(dout, route.n_tokens, dout, "dout"), _rows_arg(drows, route.n_rows, dout, "drows")
-    rs = 0 if rows is None else _rows_arg(rows, route.n_rows, dout, "rows")
+    dt, d = dout.dtype, dout.shape[-1]
+    ds, drs = _rows_arg(dout, route.n_tokens, dt, d, "dout"), _rows_arg(drows, route.n_rows, dt, d, "drows")
+    rs = 0 if rows is None else _rows_arg(rows, route.n_rows, dt, d, "rows")
     _weights_arg(weights, route, "weights")
     _weights_arg(dweights, route, "dweights")
     _ck("hl_route_combine_bwd", lib().hl_route_combine_bwd(
-        h.ptr, C.byref(route.struct), _dt(dout), dout.shape[1], _p(dout), ds, _p(rows), rs, _p(weights), _p(drows), drs,
-        _p(dweights), _s(stream)))
+        h.ptr, route.ref, _dt(dout), d, _p(dout), ds, _p(rows), rs, _p(weights), _p(drows), drs, _p(dweights), _s(stream)))
 
 
 # ------------------------------------------------------------------ clipping
