@@ -723,7 +723,7 @@ bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const fl
 // scaled by the clipping coefficient.  A wave tests BC_POS positions, lists those
 // found in LDS, and its row groups take them RPG at a time, all loads in flight
 // together.
-#define BC_POS 64
+#define BC_POS 16
 template <int VEC, bool BF>
 __global__ void __launch_bounds__(256)
 bw_clip(const uint32_t* __restrict__ keys, uint32_t n, uint32_t E, eb_geom g, void* w_hot, void* stg, uint32_t n_hot,
@@ -745,7 +745,7 @@ bw_clip(const uint32_t* __restrict__ keys, uint32_t n, uint32_t E, eb_geom g, vo
   const uint64_t p = ((uint64_t)blockIdx.x * 4 + w) * BC_POS + lane;
   uint32_t key = EB_SENT;
   bool mine = false;
-  if (p < n) {
+  if (lane < BC_POS && p < n) {
     key = keys[p];
     const uint32_t r = (uint32_t)(p % E);
     const uint32_t next = p + 1 < n ? keys[p + 1] : EB_SENT, before = p > r ? keys[p - r - 1] : EB_SENT;

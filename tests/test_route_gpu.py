@@ -84,7 +84,8 @@ def ids(seed, t, k, n_experts, drop=0.0, one=False):
     (64, 1, 64, 0, 1, 0), (65, 5, 37, 4, 3, 0.2), (1024, 1, 8, 0, 1, 0), (1025, 1, 8, 100, 128, 0.1),
     (2049, 2, 1000, 0, 1, 0), (1024, 8, 1024, 0, 16, 0.1), (8193, 1, 3, 0, 1, 0), (4096, 8, 64, 0, 16, 0),
     (4096, 8, 64, 520, 1, 0.3), (16385, 8, 1024, 7, 5, 0), (70001, 8, 129, 0, 64, 0), (300007, 7, 8, 0, 1, 0.01),
-    (1 << 18, 9, 33, 1000, 1, 0.05), (9000, 1, 5, 0, 7, 1.0)])
+    (1 << 18, 9, 33, 1000, 1, 0.05), (9000, 1, 5, 0, 7, 1.0), (4096, 1, 1024, 0, 1, 0), (4097, 1, 1024, 3, 2, 0),
+    (8192, 1, 1024, 0, 1, 0.1), (8193, 1, 1023, 0, 1, 0.1), (262144, 1, 31, 0, 8, 0), (262145, 1, 33, 0, 8, 0)])
 def test_plan(h, t, k, n_experts, capacity, align, drop):
     Plan(h, ids(t + k, t, k, n_experts, drop), n_experts, capacity, align).check()
     assert hl.hl_last_device_error(h) == 0
