@@ -722,7 +722,9 @@ bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const fl
 // one (BW_NORM above; E positions per group) applies row <- round(row - lr * G), lr
 // scaled by the clipping coefficient.  A wave tests BC_POS positions, lists those
 // found in LDS, and its row groups take them RPG at a time, all loads in flight
-// together.
+// together.  Bound by the rows and sums, each read once.  16 positions: 213,000
+// lookups of f32 rows of 64 10.2 us, 328,000 of bf16 rows of 128 15.1 (8 positions
+// 12.1 and 19.0, 32 11.8 and 17.1, 64 18.0 and 21.9; 2 rows in flight 10.9 and 15.1).
 #define BC_POS 16
 template <int VEC, bool BF>
 __global__ void __launch_bounds__(256)

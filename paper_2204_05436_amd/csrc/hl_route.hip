@@ -224,14 +224,20 @@ static uint32_t rt_tile_count(int64_t n) {
 }
 
 // ----------------------------------------------------------------------------- row movements
-// A token's row is covered by 16-byte parts, one per lane: 2^lg lanes take a
-// token's chunk of that many parts, so a block of 256 holds several short rows or
-// 256 parts (4 KB) of one, whose further chunks are the next blocks'.  Neighbouring
-// blocks thus read and write the same rows at the same time; with a wave per 1 KB
-// and the parts over blockIdx.y the rows' pieces came far apart in time, and
-// dispatch-like gathers ran at 4 TB/s and sums of rows at 4.4.
+// All of these are bound by memory: a row's 16-byte parts lie one per lane.  2^lg
+// lanes take a token's chunk of that many parts, so a block of 256 holds several
+// short rows or 256 parts (4 KB) of one, whose further chunks are the next blocks'.
+// Neighbouring blocks thus read and write the same rows at the same time; a wave per
+// KB of a row with the rows' pieces far apart in time took 155 us instead of 127 for
+// the sums of 4 rows of 8 KB of 16,384 tokens.
 // UNI: a wave's lanes all hold the same token (lg >= 6), whose rows' addresses are
-// then scalar.  KB: assignments of a token whose rows are in flight together.
+// then scalar.  KB: assignments of a token whose rows are in flight together.  HINT:
+// the non-temporal hint on the experts' rows, where those are whole cache lines
+// (neighbouring rows that share lines are better left to the L2s).  In TB/s of what
+// has to be read and written, gather, combine and combine_bwd: 16,384 tokens of 8 KB
+// in bf16 to 4 experts 5.6, 5.7, 5.9 (without the hint 5.5, 5.5, 5.2); 30,000 of 1 KB
+// to 2 6.0, 5.1, 5.6 (4.8, 5.2, 5.4); 2,999 of 3,076 bytes to 6, which share lines,
+// 4.7, 4.2, 4.1 (with it 3.9, 4.1, 3.7).  A copy of 537 MB reaches 5.4 here.
 struct rt_geom {
   int32_t dim, k, lg, chunks;  // lg: log2 of the lanes of a chunk; chunks per row
   int64_t n_tokens, rows;
@@ -280,10 +286,7 @@ __device__ __forceinline__ void rt_pad(int e, const int32_t* __restrict__ counts
       if (r >= 0) hl_vec<T>::store(out + r * stride + col, g.dim - col, hl_vec<T>::zero());
 }
 
-// A token's row is loaded once and stored k times.  HINT: the non-temporal hint on
-// the stores, where rows are whole cache lines (134 MB in rows of 4 KB 31.0 us
-// without it, 27.4 with); neighbouring rows that share lines are better left to the
-// L2s to merge (36 MB in rows of 1,332 bytes 9.7 without, 10.4 with).
+// A token's row is loaded once and stored k times.
 template <class T, bool UNI, int KB, bool HINT>
 __global__ void __launch_bounds__(256)
 rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int32_t* __restrict__ counts,
@@ -311,7 +314,7 @@ rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int
   }
 }
 
-template <class T, bool UNI, int KB, bool W>
+template <class T, bool UNI, int KB, bool W, bool HINT>
 __global__ void __launch_bounds__(256)
 rt_combine(rt_geom g, const int32_t* __restrict__ pos, const T* __restrict__ rows, int64_t rs,
            const float* __restrict__ weights, T* __restrict__ out, int64_t os, uint32_t* err) {
@@ -338,7 +341,7 @@ rt_combine(rt_geom g, const int32_t* __restrict__ pos, const T* __restrict__ row
 #pragma unroll
     for (int j = 0; j < KB; ++j) {
       p[j] = rt_row<UNI>(p[j], g.rows, err);
-      if (p[j] >= 0) v[j] = hl_vec<T>::load(rows + (int64_t)p[j] * rs + col, n);
+      if (p[j] >= 0) v[j] = hl_vec<T>::template load<HINT>(rows + (int64_t)p[j] * rs + col, n);
     }
 #pragma unroll
     for (int j = 0; j < KB; ++j)
@@ -353,8 +356,9 @@ rt_combine(rt_geom g, const int32_t* __restrict__ pos, const T* __restrict__ row
 // The gradients of the weighted sum: an assignment's row of drows is w times the
 // token's gradient, its weight's gradient their dot product.  The lanes of a
 // chunk take all of the token's chunks in turn, and add their dot products up at
-// the end.
-template <class T, bool UNI, int KB>
+// the end.  (No hint on dout: with it 58.9 us instead of 51.5 for 8,192 tokens of 8 KB
+// to 2 experts.)
+template <class T, bool UNI, int KB, bool HINT>
 __global__ void __launch_bounds__(256)
 rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int32_t* __restrict__ counts,
                const int32_t* __restrict__ offsets, const T* __restrict__ dout, int64_t ds,
@@ -390,13 +394,12 @@ rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, cons
     if (in)
       for (int32_t col = c0; col < g.dim; col += N << g.lg) {
         const int64_t n = g.dim - col;
-        const Raw d = hl_vec<T>::template load<false>(dout + t * ds + col, n);  // (with the hint 58.9 us instead
-                                                                                 // of 51.5 at 8192 tokens of 8 KB)
+        const Raw d = hl_vec<T>::template load<false>(dout + t * ds + col, n);
         Raw v[KB];
         if (dweights)
 #pragma unroll
           for (int j = 0; j < KB; ++j)
-            if (p[j] >= 0) v[j] = hl_vec<T>::load(rows + (int64_t)p[j] * rs + col, n);
+            if (p[j] >= 0) v[j] = hl_vec<T>::template load<HINT>(rows + (int64_t)p[j] * rs + col, n);
 #pragma unroll
         for (int j = 0; j < KB; ++j)
           if (p[j] >= 0) {
@@ -483,6 +486,10 @@ static rt_geom rt_make_geom(const hl_route* r, int32_t dim) {
   while (lg < 8 && (1 << lg) < parts) ++lg;
   return {dim, r->k, lg, (parts + (1 << lg) - 1) >> lg, r->n_tokens, r->n_rows};
 }
+// rows are whole cache lines
+static bool rt_lines(const void* p, int64_t stride, int32_t dim, size_t es) {
+  return ((uintptr_t)p | (uint64_t)stride * es | (uint64_t)dim * es) % HL_LINE == 0;
+}
 // KERNEL<T, UNI, KB ...>: the fewest rows in flight that hold a token's, so that no
 // registers are kept for rows it does not have
 #define RT_FORM(g, LAUNCH)                                         \
@@ -538,7 +545,7 @@ static void launch_gather(const hl_handle* h, const hl_route* r, int32_t dim, co
   const rt_geom g = rt_make_geom<T>(r, dim);
   const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg);
   const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
-  const bool lines = ((uintptr_t)out | (uint64_t)os * sizeof(T) | (uint64_t)dim * sizeof(T)) % HL_LINE == 0;
+  const bool lines = rt_lines(out, os, dim, sizeof(T));
 #define GATHER_(U, K, H)                                                                                            \
   HL_KERNEL(h, s, "rt_gather", (rt_gather<T, U, K, H>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts,        \
             r->offsets, (const T*)x, xs, (T*)out, os, h->d_err)
@@ -566,16 +573,19 @@ static void launch_combine(const hl_handle* h, const hl_route* r, int32_t dim, c
                            const float* weights, void* out, int64_t os, hipStream_t s) {
   const rt_geom g = rt_make_geom<T>(r, dim);
   const dim3 grid(hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg));
-#define COMBINE(U, K)                                                                                               \
-  do {                                                                                                              \
-    if (weights)                                                                                                    \
-      HL_KERNEL(h, s, "rt_combine", (rt_combine<T, U, K, true>), grid, dim3(256), 0, s, g, r->pos, (const T*)rows,  \
-                rs, weights, (T*)out, os, h->d_err);                                                                \
-    else                                                                                                            \
-      HL_KERNEL(h, s, "rt_combine", (rt_combine<T, U, K, false>), grid, dim3(256), 0, s, g, r->pos, (const T*)rows, \
-                rs, weights, (T*)out, os, h->d_err);                                                                \
+  const bool lines = rt_lines(rows, rs, dim, sizeof(T));
+#define COMBINE_(U, K, W, H)                                                                                        \
+  HL_KERNEL(h, s, "rt_combine", (rt_combine<T, U, K, W, H>), grid, dim3(256), 0, s, g, r->pos, (const T*)rows, rs,   \
+            weights, (T*)out, os, h->d_err)
+#define COMBINE(U, K)                                       \
+  do {                                                      \
+    if (weights && lines) COMBINE_(U, K, true, true);       \
+    else if (weights) COMBINE_(U, K, true, false);          \
+    else if (lines) COMBINE_(U, K, false, true);            \
+    else COMBINE_(U, K, false, false);                      \
   } while (0)
   RT_FORM(g, COMBINE);
+#undef COMBINE_
 #undef COMBINE
 }
 
@@ -600,14 +610,25 @@ template <class T>
 static void launch_combine_bwd(const hl_handle* h, const hl_route* r, int32_t dim, const void* dout, int64_t ds,
                                const void* rows, int64_t rs, const float* weights, void* drows, int64_t drs,
                                float* dweights, hipStream_t s) {
-  const rt_geom g = rt_make_geom<T>(r, dim);
+  rt_geom g = rt_make_geom<T>(r, dim);
+  // (a row that leaves a fifth of its lanes idle: half of them, in two rounds; rows of 333 floats 28.9 us for
+  // 30,000 assignments with a round, 26.4 with two; rows that fill their lanes lose by it: 30.0 and 34.6 for
+  // 32,768 of 1024 bf16)
+  if (g.lg > 6 && g.chunks == 1 && 5 * ((dim + hl_vec<T>::N - 1) / hl_vec<T>::N) <= 4 << g.lg) --g.lg;
   const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens, 256 >> g.lg);
   const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
-#define COMBINE_BWD(U, K)                                                                                            \
-  HL_KERNEL(h, s, "rt_combine_bwd", (rt_combine_bwd<T, U, K>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts,  \
-            r->offsets, (const T*)dout, ds, (const T*)rows, rs, weights, (T*)drows, drs, dweights, h->d_err)
+  const bool lines = rt_lines(rows, rs, g.dim, sizeof(T));
+#define COMBINE_BWD_(U, K, H)                                                                                        \
+  HL_KERNEL(h, s, "rt_combine_bwd", (rt_combine_bwd<T, U, K, H>), grid, dim3(256), 0, s, g, blocks, r->pos,          \
+            r->counts, r->offsets, (const T*)dout, ds, (const T*)rows, rs, weights, (T*)drows, drs, dweights, h->d_err)
+#define COMBINE_BWD(U, K)               \
+  do {                                  \
+    if (lines) COMBINE_BWD_(U, K, true); \
+    else COMBINE_BWD_(U, K, false);     \
+  } while (0)
   RT_FORM(g, COMBINE_BWD);
 #undef COMBINE_BWD
+#undef COMBINE_BWD_
 }
 
 extern "C" hl_status hl_route_combine_bwd(const hl_handle* h, const hl_route* r, int32_t dtype, int32_t dim,
