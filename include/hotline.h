@@ -430,8 +430,8 @@ hl_status hl_debug_ballot_ranks(hl_handle* h, int32_t on);
  * [-1, n_experts) sets HL_DEVERR_OUT_OF_RANGE and is not kept.  n_tokens may be 0.
  * Limits (HL_ERR_UNSUPPORTED): n_experts <= 1024, n_tokens*k <= 2^30, rows < 2^31.
  * HL_ERR_CAPACITY: n_rows or the workspace (hl_route_workspace_bytes; any
- * contents, NULL allowed where the call needs none: up to 8192 assignments) is
- * too small.  The handle's device must be the current one. */
+ * contents, NULL allowed where the call needs none: up to 4096 assignments) is
+ * too small.  A workspace of other calls may serve (a plan that it held is lost).  The handle's device must be the current one. */
 typedef struct hl_route {
   int64_t n_tokens;
   int32_t k;
@@ -491,9 +491,10 @@ hl_status hl_route_combine_bwd(const hl_handle* h, const hl_route* r, int32_t dt
  * 0, and n_grads too.
  * hl_grad_sq: *sq = the sum of the squares of every src (dst is not read),
  * squared and added in fp64 in an order that only the tensors' sizes fix.
- * hl_grad_clip: dst = c * src, rounded once to nearest even; with c = 0 zeros,
- * whatever src holds; dst = src (in place) or no overlap.  norm_out (device, may
- * be NULL) receives the norm.  max_norm >= 0 (infinity: never above it).
+ * hl_grad_clip: dst = c * src (c and the product in fp32, then rounded to nearest
+ * even); with c = 0 zeros, whatever src holds.  dst = src (in place) or no overlap,
+ * and no entry's dst overlaps another entry's src or dst.  norm_out (device, may be
+ * NULL) receives the norm as fp32.  max_norm >= 0 (infinity: never above it).
  * The tensors' addresses are read from the host array, which may be freed after
  * the call; a captured graph keeps them.  The workspace (hl_grad_workspace_bytes)
  * is zero-filled once before its first use (hl_workspace_init) and must not be

@@ -735,49 +735,54 @@ bw_clip(const uint32_t* __restrict__ keys, uint32_t n, uint32_t E, eb_geom g, vo
   constexpr int RPG = 4;
   __shared__ uint2 s_at[4][BC_POS];
   float norm;
-  const float coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
+  const hl_clip coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
   if (norm_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *norm_out = norm;
-  if (coef == 0.f) return;
-  lr *= coef;
+  if (coef.f == 0.f) return;
+  lr *= coef.f;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int gi = lane / g.G, gl = lane - gi * g.G;
   const int32_t colv = blockIdx.y * 64 + gl;
   const bool cact = gi < g.NG && colv < g.vpr;
   const int64_t col = (int64_t)colv * VEC;
-  const uint64_t p = ((uint64_t)blockIdx.x * 4 + w) * BC_POS + lane;
-  uint32_t key = EB_SENT;
-  bool mine = false;
-  if (lane < BC_POS && p < n) {
-    key = keys[p];
-    const uint32_t r = (uint32_t)(p % E);
-    const uint32_t next = p + 1 < n ? keys[p + 1] : EB_SENT, before = p > r ? keys[p - r - 1] : EB_SENT;
-    mine = key != EB_SENT && (r == E - 1 || next != key) && before != key;
-  }
-  const uint64_t m = __ballot(mine);
-  if (mine) s_at[w][__popcll(m & ((1ull << lane) - 1ull))] = make_uint2((uint32_t)p, key);
-  const int cnt = __popcll(m);
-  __syncthreads();
-  for (int i0 = 0; i0 < cnt; i0 += RPG * g.NG) {
-    T* row[RPG];
-    float wv[RPG][VEC], gv[RPG][VEC];
-#pragma unroll
-    for (int j = 0; j < RPG; ++j) {
-      const int i = i0 + j * g.NG + gi;
-      row[j] = nullptr;
-      if (i < cnt && cact) {
-        const uint2 a = s_at[w][i];
-        row[j] = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, a.y) + col;
-        RowIO<VEC, BF>::load(row[j], wv[j]);
-        ld_f32<VEC>(gc + (int64_t)a.x * g.D + col, gv[j]);
-      }
+  for (uint32_t b = blockIdx.x; (uint64_t)b * (4 * BC_POS) < n; b += gridDim.x) {
+    const uint32_t p = (b * 4 + w) * BC_POS + lane;  // (n < 2^30)
+    uint32_t key = EB_SENT;
+    bool mine = false;
+    if (lane < BC_POS && p < n) {
+      key = keys[p];
+      const uint32_t r = p % E;
+      const uint32_t next = p + 1 < n ? keys[p + 1] : EB_SENT, before = p > r ? keys[p - r - 1] : EB_SENT;
+      mine = key != EB_SENT && (r == E - 1 || next != key) && before != key;
     }
+    const uint64_t m = __ballot(mine);
+    const int cnt = __popcll(m);
+    // (a wave's own list: its LDS accesses keep their order, the fences hold the compiler to it)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (mine) s_at[w][__popcll(m & ((1ull << lane) - 1ull))] = make_uint2(p, key);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    for (int i0 = 0; i0 < cnt; i0 += RPG * g.NG) {
+      T* row[RPG];
+      float wv[RPG][VEC], gv[RPG][VEC];
 #pragma unroll
-    for (int j = 0; j < RPG; ++j)
-      if (row[j]) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) wv[j][e] = wv[j][e] - lr * gv[j][e];
-        RowIO<VEC, BF>::store(row[j], wv[j]);
+      for (int j = 0; j < RPG; ++j) {
+        const int i = i0 + j * g.NG + gi;
+        row[j] = nullptr;
+        if (i < cnt && cact) {
+          const uint2 a = s_at[w][i];
+          row[j] = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, a.y) + col;
+          RowIO<VEC, BF>::load(row[j], wv[j]);
+          ld_f32<VEC>(gc + (int64_t)a.x * g.D + col, gv[j]);
+        }
       }
+#pragma unroll
+      for (int j = 0; j < RPG; ++j)
+        if (row[j]) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) wv[j][e] = wv[j][e] - lr * (coef.e ? ldexpf(gv[j][e], coef.e) : gv[j][e]);
+          RowIO<VEC, BF>::store(row[j], wv[j]);
+        }
+    }
   }
 }
 
@@ -1488,10 +1493,11 @@ extern "C" hl_status hl_embbag_bwd_clip(hl_handle* h, void* w_hot, void* staging
   const int vec = eb_pick_vec(h->dim, h->dtype == HL_F32 ? 4 : 2, {w_hot, staging});
   const eb_geom g = eb_make_geom(h->dim, vec);
   const uint32_t n = none ? 0u : (uint32_t)n_lookups, E = RB_EN(rec->vec);
+  const uint32_t blocks = std::min(std::max(1u, hl_div_up(n, 4 * BC_POS)), 1u << 20);
   hipStream_t s = (hipStream_t)stream;
   const bool bf = h->dtype == HL_BF16;
 #define CLIP(V, B)                                                                                                  \
-  HL_KERNEL(h, s, "bw_clip", (bw_clip<V, B>), dim3(n ? hl_div_up(n, 4 * BC_POS) : 1, g.cchunks), dim3(256), 0, s, sk, n, E, g, \
+  HL_KERNEL(h, s, "bw_clip", (bw_clip<V, B>), dim3(blocks, g.cchunks), dim3(256), 0, s, sk, n, E, g, \
             w_hot, staging, h->n_hot, lr, ws.gc, sq, n_sq, max_norm, norm_out)
   if (vec == 8) CLIP(8, true);  // (bf16 only)
   else if (vec == 4) { if (bf) CLIP(4, true); else CLIP(4, false); }

@@ -73,9 +73,15 @@ __device__ __forceinline__ bool hl_grid_sum(double v, double* part, uint32_t* ti
 }
 
 // The norm of a step whose squares add up to sq[0] + ... + sq[n - 1], and the
-// factor that brings it to at most max_norm: 1, or max_norm / norm, or 0 where
-// the norm is not finite.  The same on every lane; every lane of a wave calls it.
-__device__ __forceinline__ float hl_clip_coef(const double* sq, int32_t n, float max_norm, float* norm) {
+// factor c that brings it to at most max_norm: 1, or max_norm / norm, or 0 where the
+// norm is not finite.  As f * 2^e, e = 0 unless c is so small that fp32 would hold it
+// with fewer bits or not at all (the norm may pass 1e38).
+// The same on every lane; every lane of a wave calls it.
+struct hl_clip {
+  float f;
+  int e;
+};
+__device__ __forceinline__ hl_clip hl_clip_coef(const double* sq, int32_t n, float max_norm, float* norm) {
   double s = 0.;
   if (n <= 64) {  // (uniform: few terms, in order)
     for (int32_t i = 0; i < n; ++i) s += sq[i];
@@ -85,6 +91,11 @@ __device__ __forceinline__ float hl_clip_coef(const double* sq, int32_t n, float
   }
   const double d = sqrt(s);
   *norm = (float)d;
-  if (!(d <= 1.7976931348623157e308)) return 0.f;
-  return d > (double)max_norm ? (float)((double)max_norm / d) : 1.f;
+  if (!(d <= 1.7976931348623157e308)) return {0.f, 0};
+  if (!(d > (double)max_norm)) return {1.f, 0};
+  const double c = (double)max_norm / d;
+  if (c >= 0x1p-100 || c == 0.) return {(float)c, 0};
+  int e;
+  const double m = frexp(c, &e);
+  return {(float)m, e};
 }

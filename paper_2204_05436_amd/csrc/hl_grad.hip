@@ -100,7 +100,7 @@ gr_sq(gr_sq_args g, double* part, uint32_t* ticket, double* out, uint32_t* err) 
 }
 
 template <class T, class A = gr_clip_args>
-__device__ __forceinline__ void gr_scale(const void* src, void* dst, uint32_t n, uint32_t c, float coef) {
+__device__ __forceinline__ void gr_scale(const void* src, void* dst, uint32_t n, uint32_t c, hl_clip coef) {
   constexpr int N = hl_vec<T>::N;
   const T* p = (const T*)src;
   T* q = (T*)dst;
@@ -116,7 +116,10 @@ __device__ __forceinline__ void gr_scale(const void* src, void* dst, uint32_t n,
     const uint32_t i = i0 + k * 256 * N;
     float o[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) o[j] = coef == 0.f ? 0.f : (float)v[k][j] * coef;
+    for (int j = 0; j < N; ++j) {
+      o[j] = coef.f == 0.f ? 0.f : (float)v[k][j] * coef.f;
+      if (coef.e) o[j] = ldexpf(o[j], coef.e);
+    }
     if (i < n) hl_vec<T>::store(q + i, n - i, hl_vec<T>::pack(o));
   }
 }
@@ -129,14 +132,14 @@ gr_clip(gr_clip_args g, const double* __restrict__ sq, int32_t n_sq, float max_n
   const gr_find<gr_clip_args> find(g);
   const int t0 = find(g.chunks - 1 - blockIdx.x);
   float norm;
-  const float coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
+  const hl_clip coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
   for (uint32_t i = blockIdx.x; i < g.chunks; i += gridDim.x) {
     const uint32_t c = g.chunks - 1 - i;
     const int t = i == blockIdx.x ? t0 : find(c);
     const uint32_t n = g.n[t];
     const uint32_t at = c - g.c0[t];
-    if (coef == 1.f && g.src[t] == g.dst[t]) continue;
+    if (coef.f == 1.f && coef.e == 0 && g.src[t] == g.dst[t]) continue;
     if ((n & 3) == HL_F32) gr_scale<float>(g.src[t], g.dst[t], n >> 2, at, coef);
     else if ((n & 3) == HL_BF16) gr_scale<__bf16>(g.src[t], g.dst[t], n >> 2, at, coef);
     else gr_scale<_Float16>(g.src[t], g.dst[t], n >> 2, at, coef);

@@ -241,18 +241,21 @@ static uint32_t rt_tile_count(int64_t n) {
 struct rt_geom {
   int32_t dim, k, lg, chunks;  // lg: log2 of the lanes of a chunk; chunks per row
   int64_t n_tokens, rows;
+  int32_t n_experts;
 };
 
+// Blocks in x and y together: a grid's x may not hold more than 2^32 threads.
+__device__ __forceinline__ uint32_t rt_block() { return blockIdx.x + blockIdx.y * gridDim.x; }
 // This lane's token and column; false: none.
 template <class T, bool UNI>
 __device__ __forceinline__ bool rt_part(const rt_geom& g, uint32_t* t, int32_t* col) {
   uint32_t u, l;
   if (UNI) {
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    u = blockIdx.x * (256u >> g.lg) + (w >> (g.lg - 6));
+    u = rt_block() * (256u >> g.lg) + (w >> (g.lg - 6));
     l = ((w & ((1u << (g.lg - 6)) - 1)) << 6) + (threadIdx.x & 63);
   } else {
-    u = blockIdx.x * (256u >> g.lg) + (threadIdx.x >> g.lg);
+    u = rt_block() * (256u >> g.lg) + (threadIdx.x >> g.lg);
     l = threadIdx.x & ((1u << g.lg) - 1);
   }
   uint32_t c = 0;
@@ -276,14 +279,15 @@ __device__ __forceinline__ int32_t rt_row(int32_t p, int64_t rows, uint32_t* err
 }
 // The padding rows of expert e's block, set to zero.
 template <class T>
-__device__ __forceinline__ void rt_pad(int e, const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
-                                       const rt_geom& g, T* __restrict__ out, int64_t stride) {
+__device__ __forceinline__ void rt_pad(uint32_t e, const int32_t* __restrict__ counts,
+                                       const int32_t* __restrict__ offsets, const rt_geom& g, T* __restrict__ out,
+                                       int64_t stride) {
   constexpr int N = hl_vec<T>::N;
+  if (e >= (uint32_t)g.n_experts) return;
   const int64_t end = min((int64_t)offsets[e + 1], g.rows);
-  const int lg = min(g.lg, 8);
-  for (int64_t r = (int64_t)offsets[e] + counts[e] + (threadIdx.x >> lg); r < end; r += 256 >> lg)
-    for (int64_t col = (int64_t)(threadIdx.x & ((1 << lg) - 1)) * N; col < g.dim; col += (int64_t)N << lg)
-      if (r >= 0) hl_vec<T>::store(out + r * stride + col, g.dim - col, hl_vec<T>::zero());
+  for (int64_t r = max((int64_t)offsets[e] + counts[e], (int64_t)0) + (threadIdx.x >> g.lg); r < end; r += 256 >> g.lg)
+    for (int64_t col = (int64_t)(threadIdx.x & ((1 << g.lg) - 1)) * N; col < g.dim; col += (int64_t)N << g.lg)
+      hl_vec<T>::store(out + r * stride + col, g.dim - col, hl_vec<T>::zero());
 }
 
 // A token's row is loaded once and stored k times.
@@ -292,8 +296,8 @@ __global__ void __launch_bounds__(256)
 rt_gather(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, const int32_t* __restrict__ counts,
           const int32_t* __restrict__ offsets, const T* __restrict__ x, int64_t xs, T* __restrict__ out, int64_t os,
           uint32_t* err) {
-  if (blockIdx.x >= blocks) {
-    rt_pad<T>(blockIdx.x - blocks, counts, offsets, g, out, os);
+  if (rt_block() >= blocks) {
+    rt_pad<T>(rt_block() - blocks, counts, offsets, g, out, os);
     return;
   }
   uint32_t t;
@@ -367,8 +371,8 @@ rt_combine_bwd(rt_geom g, uint32_t blocks, const int32_t* __restrict__ pos, cons
   typedef typename hl_vec<T>::Raw Raw;
   constexpr int N = hl_vec<T>::N;
   __shared__ float s_dot[4][KB];
-  if (blockIdx.x >= blocks) {
-    rt_pad<T>(blockIdx.x - blocks, counts, offsets, g, drows, drs);
+  if (rt_block() >= blocks) {
+    rt_pad<T>(rt_block() - blocks, counts, offsets, g, drows, drs);
     return;
   }
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -448,7 +452,9 @@ extern "C" int64_t hl_route_rows(int64_t n_tokens, int32_t k, int32_t n_experts,
 extern "C" size_t hl_route_workspace_bytes(int64_t n_tokens, int32_t k, int32_t n_experts) {
   if (n_tokens < 0 || k < 1 || n_experts < 1 || n_experts > RT_MAX_EXPERTS) return 0;
   if (n_tokens > (1ll << 30) || n_tokens * k > (1ll << 30)) return 0;
-  return (((size_t)rt_tile_count(n_tokens * k) + 1) * n_experts * 4 + 255) & ~(size_t)255;
+  hl_carver c = hl_carver::after_header(nullptr, 0);
+  c.take<uint32_t>(((size_t)rt_tile_count(n_tokens * k) + 1) * n_experts);
+  return (c.off + 255) & ~(size_t)255;
 }
 
 static hl_status rt_check(const hl_handle* h, const hl_route* r) {
@@ -484,7 +490,11 @@ static rt_geom rt_make_geom(const hl_route* r, int32_t dim) {
   const int parts = (dim + hl_vec<T>::N - 1) / hl_vec<T>::N;
   int lg = 0;
   while (lg < 8 && (1 << lg) < parts) ++lg;
-  return {dim, r->k, lg, (parts + (1 << lg) - 1) >> lg, r->n_tokens, r->n_rows};
+  return {dim, r->k, lg, (parts + (1 << lg) - 1) >> lg, r->n_tokens, r->n_rows, r->n_experts};
+}
+#define RT_GRID_X (1u << 20)
+static dim3 rt_grid(uint64_t blocks) {
+  return blocks <= RT_GRID_X ? dim3((uint32_t)blocks) : dim3(RT_GRID_X, hl_div_up(blocks, RT_GRID_X));
 }
 // rows are whole cache lines
 static bool rt_lines(const void* p, int64_t stride, int32_t dim, size_t es) {
@@ -516,7 +526,9 @@ extern "C" hl_status hl_route_plan(hl_handle* h, const hl_route* r, const int32_
   if (tiles > 1 && (!workspace || (uintptr_t)workspace % 4 != 0)) return HL_ERR_INVALID_ARG;
   if (tiles > 1 && ws_bytes < hl_route_workspace_bytes(r->n_tokens, r->k, r->n_experts)) return HL_ERR_CAPACITY;
   hipStream_t s = (hipStream_t)stream;
-  uint32_t* hist = (uint32_t*)workspace;
+  // (past the header, whose counters other calls on this workspace keep)
+  hl_carver c = hl_carver::after_header(workspace, ws_bytes);
+  uint32_t* hist = workspace ? c.take<uint32_t>(1) : nullptr;
   if (workspace) hl_ws_note(h, workspace, HL_WSK_OTHER);
   const int bits = r->n_experts > 1 ? hl_bit_width((uint64_t)r->n_experts - 1) : 0;
   const rt_shape sh = {(int32_t)n,  r->n_experts, bits, r->capacity ? r->capacity : INT32_MAX, r->align,
@@ -544,7 +556,7 @@ static void launch_gather(const hl_handle* h, const hl_route* r, int32_t dim, co
                           int64_t os, hipStream_t s) {
   const rt_geom g = rt_make_geom<T>(r, dim);
   const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg);
-  const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
+  const dim3 grid = rt_grid((uint64_t)blocks + (r->align > 1 ? r->n_experts : 0));
   const bool lines = rt_lines(out, os, dim, sizeof(T));
 #define GATHER_(U, K, H)                                                                                            \
   HL_KERNEL(h, s, "rt_gather", (rt_gather<T, U, K, H>), grid, dim3(256), 0, s, g, blocks, r->pos, r->counts,        \
@@ -572,7 +584,7 @@ template <class T>
 static void launch_combine(const hl_handle* h, const hl_route* r, int32_t dim, const void* rows, int64_t rs,
                            const float* weights, void* out, int64_t os, hipStream_t s) {
   const rt_geom g = rt_make_geom<T>(r, dim);
-  const dim3 grid(hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg));
+  const dim3 grid = rt_grid(hl_div_up((uint64_t)g.n_tokens * g.chunks, 256 >> g.lg));
   const bool lines = rt_lines(rows, rs, dim, sizeof(T));
 #define COMBINE_(U, K, W, H)                                                                                        \
   HL_KERNEL(h, s, "rt_combine", (rt_combine<T, U, K, W, H>), grid, dim3(256), 0, s, g, r->pos, (const T*)rows, rs,   \
@@ -616,7 +628,7 @@ static void launch_combine_bwd(const hl_handle* h, const hl_route* r, int32_t di
   // 32,768 of 1024 bf16)
   if (g.lg > 6 && g.chunks == 1 && 5 * ((dim + hl_vec<T>::N - 1) / hl_vec<T>::N) <= 4 << g.lg) --g.lg;
   const uint32_t blocks = hl_div_up((uint64_t)g.n_tokens, 256 >> g.lg);
-  const dim3 grid(blocks + (r->align > 1 ? r->n_experts : 0));
+  const dim3 grid = rt_grid((uint64_t)blocks + (r->align > 1 ? r->n_experts : 0));
   const bool lines = rt_lines(rows, rs, g.dim, sizeof(T));
 #define COMBINE_BWD_(U, K, H)                                                                                        \
   HL_KERNEL(h, s, "rt_combine_bwd", (rt_combine_bwd<T, U, K, H>), grid, dim3(256), 0, s, g, blocks, r->pos,          \

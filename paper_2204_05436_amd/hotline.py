@@ -618,6 +618,19 @@ class GradList:
             if not g.is_contiguous() or not d.is_contiguous() or d.dtype != g.dtype or d.numel() != g.numel():
                 raise ValueError("gradients and their outputs: contiguous, of the same type and size")
             a.src, a.dst, a.n, a.dtype = _p(g), _p(d), g.numel(), _dt(g)
+        # an output that another entry reads or writes would be scaled before, after or twice
+        spans = []
+        for a in self.array[:len(self.grads)]:
+            size = a.n * (4 if a.dtype == HL_F32 else 2)
+            for p in {a.src, a.dst} if size else ():
+                spans.append((p, p + size, p == a.dst))
+        end = written = 0  # the furthest end so far, of all and of outputs
+        for lo, hi, out in sorted(spans):
+            if lo < (end if out else written):
+                raise ValueError("an entry's output overlaps another entry")
+            end = max(end, hi)
+            if out:
+                written = max(written, hi)
 
     def __len__(self):
         return len(self.grads)

@@ -133,8 +133,8 @@ def test_extremes(h, ws, dt):
         want = float(t[0].double()) * math.sqrt(333)
         hl.hl_grad_sq(h, hl.GradList([t]), sq, ws)
         assert sq_ok(float(sq), want * want)
-        for max_norm in (want / 2, 0.0, math.inf):
-            m = float(np.float32(max_norm))
+        for max_norm in (want / 2, 0.0, math.inf, 1.0, 1e-6, 1e-30):
+            m = math.inf if max_norm > 3e38 else float(np.float32(max_norm))
             out = torch.empty_like(t)
             hl.hl_grad_clip(h, hl.GradList([t], [out]), sq, m, norm)
             assert clipped_ok(t, out, coef(want, m))

@@ -111,6 +111,15 @@ def test_binding_refuses_gradients():
             hl.GradList(g, o)
     with pytest.raises(TypeError):
         hl.GradList([torch.zeros(4, dtype=torch.float64)])
+    # the same tensor twice, or an output inside what another entry reads or writes
+    x, y = torch.zeros(16), torch.zeros(16)
+    for g, o in [([x, x], None), ([x[:8], x[4:12]], None), ([x, x[2:4]], None), ([x[:8], x[8:]], [y[:8], x[:8]]),
+                 ([x[:8], x[8:]], [y[:8], y[7:15]]), ([x[:8]], [x[4:12]]), ([x, y[:4]], [y, y[:4]])]:
+        with pytest.raises(ValueError):
+            hl.GradList(g, o)
+    for g, o in [([x[:8], x[8:]], None), ([x[:8], x[8:]], [y[:8], y[8:]]), ([x, x[:0]], None), ([x, x], [y, torch.zeros(16)]),
+                 ([x[:8], x[8:]], [x[:8], y[:8]]), ([x[:8], x[8:], y], [x[:8], x[8:], y])]:
+        hl.GradList(g, o)
     with pytest.raises(ValueError):
         hl.hl_grad_sq(_Handle(), hl.GradList([a]), torch.zeros(1), torch.zeros(8, dtype=torch.uint8), stream=0)
     with pytest.raises(ValueError):

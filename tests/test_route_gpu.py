@@ -287,6 +287,66 @@ def test_far_rows(h):
     assert hl.hl_last_device_error(h) == 0
 
 
+def test_many_blocks(h):
+    """More blocks than one dimension of a grid is given (2^20): the second one counts."""
+    t, dim, E = (1 << 20) + 70_001, 1024, 3
+    e = torch.randint(-1, E, (t, 1), dtype=torch.int32, generator=torch.Generator().manual_seed(1))
+    p = Plan(h, e, E, align=64, order=False)
+    p.check()
+    x = torch.empty(t, dim, dtype=torch.float32, device="cuda")
+    x.copy_(torch.arange(t, dtype=torch.float32, device="cuda")[:, None])  # (every row its number, below 2^24)
+    rows = torch.full((p.n_rows, dim), -5.0, device="cuda")
+    hl.hl_route_gather(h, p.route, x, rows)
+    pos = p.pos.long()
+    kept = (pos >= 0).nonzero().view(-1)
+    want = torch.full((p.n_rows,), 0.0, device="cuda")
+    want[pos[kept]] = kept.float()
+    want[int(p.offsets[-1]):] = -5.0
+    assert bool((rows == want[:, None]).all())
+    hl.hl_route_combine(h, p.route, rows, torch.full((t, 1), 2.0, device="cuda"), x)
+    want = torch.zeros(t, device="cuda")
+    want[kept] = 2.0 * kept.float()
+    assert bool((x == want[:, None]).all())
+    dw = torch.full((t, 1), 9.0, device="cuda")
+    hl.hl_route_combine_bwd(h, p.route, x, rows, None, rows.new_zeros(rows.shape), dw)
+    ref = torch.zeros(t, dtype=torch.float64, device="cuda")
+    ref[kept] = 2.0 * kept.double() ** 2 * dim
+    assert ((dw.view(-1).double() - ref).abs() <= 2 * (4 * 4 + 10) * U * ref).all()
+    assert hl.hl_last_device_error(h) == 0
+
+
+def test_workspace_of_other_calls():
+    """A workspace that other calls use serves the plan too, and serves them afterwards (its header's counters stay)."""
+    T, B, L = 2, 3000, 6000
+    h = hl.hl_create([500] * T, 8, "f32", 100)
+    try:
+        hl.hl_set_hot(h, torch.arange(0, 1000, 10, dtype=torch.int32, device="cuda"), 100)
+        r = torch.randint(0, 500, (L,), dtype=torch.int32, generator=torch.Generator().manual_seed(3)).cuda()
+        ptr = torch.arange(L + 1, dtype=torch.int32, device="cuda")
+        t, k, E = 20000, 2, 300
+        size = max(hl.hl_workspace_bytes(h, L, L, B), hl.hl_route_workspace_bytes(t, k, E), hl.hl_grad_workspace_bytes())
+        ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+        i32 = dict(dtype=torch.int32, device="cuda")
+        first = None
+        for turn in range(4):
+            out = [torch.zeros(n, **i32) for n in (L, L)] + [torch.zeros(B, dtype=torch.uint8, device="cuda")]
+            lists = [torch.zeros(n, **i32) for n in (B, B, 2)]
+            hl.hl_dispatch(h, r, ptr, B, T, L, *out, *lists, ws)
+            assert hl.hl_last_device_error(h) == 0
+            got = [x.clone() for x in out + lists]
+            first = first or got
+            assert all(torch.equal(a, b) for a, b in zip(first, got))
+            p = Plan(h, ids(turn, t, k, E), E)
+            hl.hl_route_plan(h, p.route, p.experts, ws)
+            p.check()
+            g = torch.full((300_000 * (1 + 20 * (turn % 2)),), 0.5, device="cuda")  # (few and many blocks)
+            sq = torch.zeros(1, dtype=torch.float64, device="cuda")
+            hl.hl_grad_sq(h, hl.GradList([g]), sq, ws)
+            assert float(sq) == 0.25 * g.numel()
+    finally:
+        h.close()
+
+
 def test_refusals(h):
     p = Plan(h, ids(0, 4, 2, 3), 3, align=2)
     r, L = p.route, hl.lib()
