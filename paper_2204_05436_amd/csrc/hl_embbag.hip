@@ -722,9 +722,10 @@ bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const fl
 // one (BW_NORM above; E positions per group) applies row <- round(row - lr * G), lr
 // scaled by the clipping coefficient.  A wave tests BC_POS positions, lists those
 // found in LDS, and its row groups take them RPG at a time, all loads in flight
-// together.  Bound by the rows and sums, each read once.  16 positions: 213,000
-// lookups of f32 rows of 64 10.2 us, 328,000 of bf16 rows of 128 15.1 (8 positions
-// 12.1 and 19.0, 32 11.8 and 17.1, 64 18.0 and 21.9; 2 rows in flight 10.9 and 15.1).
+// together.  Bound by the rows and sums, each read once: 213,000 lookups of f32 rows
+// of 64 11.0 us, 328,000 of bf16 rows of 128 15.9.  (Before the factor's exponent
+// came in, 16 positions 10.2 and 15.1, 8 12.1 and 19.0, 32 11.8 and 17.1, 64 18.0 and
+// 21.9; 2 rows in flight 10.9 and 15.1.)
 #define BC_POS 16
 template <int VEC, bool BF>
 __global__ void __launch_bounds__(256)
@@ -736,7 +737,7 @@ bw_clip(const uint32_t* __restrict__ keys, uint32_t n, uint32_t E, eb_geom g, vo
   __shared__ uint2 s_at[4][BC_POS];
   float norm;
   const hl_clip coef = hl_clip_coef(sq, n_sq, max_norm, &norm);
-  if (norm_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *norm_out = norm;
+  if (norm_out && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) *norm_out = norm;
   if (coef.f == 0.f) return;
   lr *= coef.f;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -744,45 +745,47 @@ bw_clip(const uint32_t* __restrict__ keys, uint32_t n, uint32_t E, eb_geom g, vo
   const int32_t colv = blockIdx.y * 64 + gl;
   const bool cact = gi < g.NG && colv < g.vpr;
   const int64_t col = (int64_t)colv * VEC;
-  for (uint32_t b = blockIdx.x; (uint64_t)b * (4 * BC_POS) < n; b += gridDim.x) {
-    const uint32_t p = (b * 4 + w) * BC_POS + lane;  // (n < 2^30)
-    uint32_t key = EB_SENT;
-    bool mine = false;
-    if (lane < BC_POS && p < n) {
-      key = keys[p];
-      const uint32_t r = p % E;
-      const uint32_t next = p + 1 < n ? keys[p + 1] : EB_SENT, before = p > r ? keys[p - r - 1] : EB_SENT;
-      mine = key != EB_SENT && (r == E - 1 || next != key) && before != key;
-    }
-    const uint64_t m = __ballot(mine);
-    const int cnt = __popcll(m);
-    // (a wave's own list: its LDS accesses keep their order, the fences hold the compiler to it)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (mine) s_at[w][__popcll(m & ((1ull << lane) - 1ull))] = make_uint2(p, key);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    for (int i0 = 0; i0 < cnt; i0 += RPG * g.NG) {
-      T* row[RPG];
-      float wv[RPG][VEC], gv[RPG][VEC];
+  const uint32_t b = blockIdx.x + blockIdx.z * gridDim.x;  // (a grid's x may not hold more than 2^32 threads)
+  const uint32_t p = (b * 4 + w) * BC_POS + lane;  // (n < 2^30)
+  uint32_t key = EB_SENT;
+  bool mine = false;
+  if (lane < BC_POS && p < n) {
+    key = keys[p];
+    const uint32_t r = p % E;
+    const uint32_t next = p + 1 < n ? keys[p + 1] : EB_SENT, before = p > r ? keys[p - r - 1] : EB_SENT;
+    mine = key != EB_SENT && (r == E - 1 || next != key) && before != key;
+  }
+  const uint64_t m = __ballot(mine);
+  const int cnt = __popcll(m);
+  // (a wave's own list: its LDS accesses keep their order, the fences hold the compiler to it)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (mine) s_at[w][__popcll(m & ((1ull << lane) - 1ull))] = make_uint2(p, key);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  for (int i0 = 0; i0 < cnt; i0 += RPG * g.NG) {
+    T* row[RPG];
+    typename RowIO<VEC, BF>::Raw wr[RPG];
+    float gv[RPG][VEC];
 #pragma unroll
-      for (int j = 0; j < RPG; ++j) {
-        const int i = i0 + j * g.NG + gi;
-        row[j] = nullptr;
-        if (i < cnt && cact) {
-          const uint2 a = s_at[w][i];
-          row[j] = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, a.y) + col;
-          RowIO<VEC, BF>::load(row[j], wv[j]);
-          ld_f32<VEC>(gc + (int64_t)a.x * g.D + col, gv[j]);
-        }
+    for (int j = 0; j < RPG; ++j) {
+      const int i = i0 + j * g.NG + gi;
+      row[j] = nullptr;
+      if (i < cnt && cact) {
+        const uint2 a = s_at[w][i];
+        row[j] = bw_row<VEC, BF>(w_hot, stg, n_hot, g.D, a.y) + col;
+        wr[j] = RowIO<VEC, BF>::load_raw(row[j]);
+        ld_f32<VEC>(gc + (int64_t)a.x * g.D + col, gv[j]);
       }
-#pragma unroll
-      for (int j = 0; j < RPG; ++j)
-        if (row[j]) {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) wv[j][e] = wv[j][e] - lr * (coef.e ? ldexpf(gv[j][e], coef.e) : gv[j][e]);
-          RowIO<VEC, BF>::store(row[j], wv[j]);
-        }
     }
+#pragma unroll
+    for (int j = 0; j < RPG; ++j)
+      if (row[j]) {
+        float wv[VEC];
+        RowIO<VEC, BF>::unpack(wr[j], wv);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) wv[e] = wv[e] - lr * (coef.e ? ldexpf(gv[j][e], coef.e) : gv[j][e]);
+        RowIO<VEC, BF>::store(row[j], wv);
+      }
   }
 }
 
@@ -1493,11 +1496,11 @@ extern "C" hl_status hl_embbag_bwd_clip(hl_handle* h, void* w_hot, void* staging
   const int vec = eb_pick_vec(h->dim, h->dtype == HL_F32 ? 4 : 2, {w_hot, staging});
   const eb_geom g = eb_make_geom(h->dim, vec);
   const uint32_t n = none ? 0u : (uint32_t)n_lookups, E = RB_EN(rec->vec);
-  const uint32_t blocks = std::min(std::max(1u, hl_div_up(n, 4 * BC_POS)), 1u << 20);
+  const uint32_t blocks = std::max(1u, hl_div_up(n, 4 * BC_POS)), bz = hl_div_up(blocks, 1u << 20);
   hipStream_t s = (hipStream_t)stream;
   const bool bf = h->dtype == HL_BF16;
 #define CLIP(V, B)                                                                                                  \
-  HL_KERNEL(h, s, "bw_clip", (bw_clip<V, B>), dim3(blocks, g.cchunks), dim3(256), 0, s, sk, n, E, g, \
+  HL_KERNEL(h, s, "bw_clip", (bw_clip<V, B>), dim3(hl_div_up(blocks, bz), g.cchunks, bz), dim3(256), 0, s, sk, n, E, g, \
             w_hot, staging, h->n_hot, lr, ws.gc, sq, n_sq, max_norm, norm_out)
   if (vec == 8) CLIP(8, true);  // (bf16 only)
   else if (vec == 4) { if (bf) CLIP(4, true); else CLIP(4, false); }

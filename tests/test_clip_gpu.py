@@ -355,6 +355,36 @@ def test_tables_gradient_by_differences():
         t.h.close()
 
 
+def test_tables_many_lookups():
+    """More lookups than one dimension of the clipped update's grid takes (2^26), of few rows and of many."""
+    L, bags, n_hot, n_stg = (1 << 26) + 4_000_003, 1000, 30_000_000, 5
+    h = hl.hl_create([n_hot + 100], 1, "f32", n_hot)
+    try:
+        hl.hl_set_hot(h, torch.arange(n_hot, dtype=torch.int32, device="cuda"), n_hot)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        codes = torch.randint(0, n_hot + n_stg, (L,), dtype=torch.int32, device="cuda", generator=g)
+        codes[: L // 4] %= 100  # (long runs)
+        ptr = torch.linspace(0, L, bags + 1, dtype=torch.float64, device="cuda").to(torch.int32)
+        dY = torch.randint(-4, 5, (bags, 1), device="cuda", generator=g).float()
+        ws = torch.zeros(hl.hl_workspace_bytes(h, L, bags, bags), dtype=torch.uint8, device="cuda")
+        sq = torch.zeros(1, dtype=torch.float64, device="cuda")
+        a = torch.randn(n_hot + n_stg, 1, device="cuda", generator=g)
+        b = a.clone()
+        shape = (n_stg, bags, 1, L)
+        hl.hl_embbag_bwd_plan(h, n_stg, codes, ptr, bags, 1, L, None, None, bags, ws)
+        hl.hl_embbag_bwd_norm(h, *shape, dY, sq, ws)
+        bag = torch.repeat_interleave(torch.arange(bags, device="cuda"), (ptr[1:] - ptr[:-1]).long())
+        G = torch.zeros(n_hot + n_stg, dtype=torch.float64, device="cuda").index_add_(0, codes, dY.double()[bag, 0])
+        assert float(G.abs().max()) < 2 ** 24  # (whole numbers: exact sums)
+        assert sq_ok(float(sq), float(G.square().sum()))
+        hl.hl_embbag_bwd_clip(h, a[:n_hot], a[n_hot:], *shape, sq, math.inf, 0.5, ws)
+        hl.hl_embbag_bwd_apply(h, b[:n_hot], b[n_hot:], *shape, dY, 0.5, ws)
+        assert torch.equal(a, b)
+        assert hl.hl_last_device_error(h) == 0
+    finally:
+        h.close()
+
+
 def test_tables_unaligned_rows():
     """Rows and gradients at addresses that allow narrower loads only."""
     t = Tables(3, 400, 64, "f32", 150, 2.0, seed=5)
