@@ -90,8 +90,8 @@ uint32_t hl_k_cap(const hl_handle* h);
  * max_samples samples.  A workspace must be zero-filled once before its first
  * use (hl_workspace_init, or any zero fill) and then belongs to this handle;
  * the calls keep it reusable.  Used by hl_partition, hl_cold_plan /
- * hl_cold_gather and hl_embbag_bwd_plan / _apply / _sgd, never two of them
- * concurrently; hl_cold_fetch and hl_cold_scatter do not touch it. */
+ * hl_cold_gather and hl_embbag_bwd_plan / _apply / _sgd / _norm / _clip, never two
+ * of them concurrently; hl_cold_fetch and hl_cold_scatter do not touch it. */
 size_t hl_workspace_bytes(const hl_handle* h, int64_t max_lookups, int64_t max_bags,
                           int32_t max_samples);
 hl_status hl_workspace_init(void* workspace, size_t bytes, hl_stream stream);

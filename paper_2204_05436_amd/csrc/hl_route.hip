@@ -479,7 +479,8 @@ static hl_status rt_check_rows(const hl_handle* h, const hl_route* r, int32_t dt
   if (st != HL_OK) return st;
   const size_t es = hl_elem_bytes(dtype);
   if (!es || dim < 1) return HL_ERR_INVALID_ARG;
-  if (dim > RT_MAX_DIM) return HL_ERR_UNSUPPORTED;
+  // (blocks of 4 KB of a row: fewer than 2^31, 8 TB of tokens)
+  if (dim > RT_MAX_DIM || r->n_tokens * (int64_t)hl_div_up(dim * es, 4096) >= (1ll << 31)) return HL_ERR_UNSUPPORTED;
   if (r->n_tokens == 0) return HL_OK;
   st = rt_rows_ok(a, as, dim, es);
   return st != HL_OK ? st : rt_rows_ok(b, bs, dim, es);

@@ -219,9 +219,16 @@ def _nbytes(t):
     return t.numel() * t.element_size()
 
 
+_plain = {}  # "int32" -> torch.int32, ...
+
+
 def _check_plain(x, dtype, n, what):
     """x holds n contiguous elements of dtype (a torch type's name)."""
-    if str(x.dtype) != "torch." + dtype or not x.is_contiguous() or x.numel() < n:
+    t = _plain.get(dtype)
+    if t is None:
+        import torch
+        t = _plain[dtype] = getattr(torch, dtype)
+    if x.dtype is not t or x.numel() < n or not x.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous {dtype} elements wanted, got {x.dtype} {tuple(x.shape)}")
 
 
@@ -553,7 +560,7 @@ class Route:
 def _rows_arg(x, rows, dtype, dim, what):
     """The stride of a row buffer: at least `rows` rows of dim contiguous elements of dtype."""
     shape, stride = x.shape, x.stride()
-    if len(shape) != 2 or x.dtype != dtype or shape[1] != dim or shape[0] < rows or (dim > 1 and stride[1] != 1):
+    if len(shape) != 2 or x.dtype is not dtype or shape[1] != dim or shape[0] < rows or (dim > 1 and stride[1] != 1):
         raise ValueError(f"{what}: {rows} rows of {dim} contiguous {dtype} elements wanted, got {tuple(shape)} {x.dtype} "
                          f"with strides {stride}")
     return stride[0] if shape[0] > 1 else max(stride[0], dim)
@@ -566,29 +573,30 @@ def _weights_arg(w, route, what):
 
 def hl_route_plan(h, route, experts, ws=None, stream=None):
     _check_plain(experts, "int32", route.n_tokens * route.k, "experts")
-    _ck("hl_route_plan", lib().hl_route_plan(h.ptr, route.ref, _p(experts), _p(ws), 0 if ws is None else _nbytes(ws),
-                                             _s(stream)))
+    _ck("hl_route_plan", lib().hl_route_plan(h.ptr, route.ref, experts.data_ptr(), _p(ws),
+                                             0 if ws is None else _nbytes(ws), _s(stream)))
 
 
 def hl_route_gather(h, route, x, rows, stream=None):
     dt, d = x.dtype, x.shape[-1]
     xs, rs = _rows_arg(x, route.n_tokens, dt, d, "x"), _rows_arg(rows, route.n_rows, dt, d, "rows")
-    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, route.ref, _dt(x), d, _p(x), xs, _p(rows), rs, _s(stream)))
+    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, route.ref, _dt(x), d, x.data_ptr(), xs, rows.data_ptr(), rs,
+                                                 _s(stream)))
 
 
 def hl_route_gather_bwd(h, route, drows, dx, stream=None):
     dt, d = drows.dtype, drows.shape[-1]
     rs, xs = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx")
-    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, _dt(drows), d, _p(drows), rs, _p(dx), xs,
-                                                         _s(stream)))
+    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, _dt(drows), d, drows.data_ptr(), rs,
+                                                         dx.data_ptr(), xs, _s(stream)))
 
 
 def hl_route_combine(h, route, rows, weights, out, stream=None):
     dt, d = rows.dtype, rows.shape[-1]
     rs, os_ = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out")
     _weights_arg(weights, route, "weights")
-    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, route.ref, _dt(rows), d, _p(rows), rs, _p(weights), _p(out), os_,
-                                                   _s(stream)))
+    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, route.ref, _dt(rows), d, rows.data_ptr(), rs, _p(weights),
+                                                   out.data_ptr(), os_, _s(stream)))
 
 
 def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, stream=None):
@@ -599,7 +607,8 @@ def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, st
     _weights_arg(weights, route, "weights")
     _weights_arg(dweights, route, "dweights")
     _ck("hl_route_combine_bwd", lib().hl_route_combine_bwd(
-        h.ptr, route.ref, _dt(dout), d, _p(dout), ds, _p(rows), rs, _p(weights), _p(drows), drs, _p(dweights), _s(stream)))
+        h.ptr, route.ref, _dt(dout), d, dout.data_ptr(), ds, _p(rows), rs, _p(weights), drows.data_ptr(), drs,
+        _p(dweights), _s(stream)))
 
 
 # ------------------------------------------------------------------ clipping

@@ -97,6 +97,46 @@ def test_dense(h, ws, sizes, dtypes, shift):
     assert hl.hl_last_device_error(h) == 0
 
 
+def test_long_tensor(h, ws):
+    """A tensor of more elements than one entry of a launch takes (2^29), at an odd address."""
+    n = (1 << 29) + 12_345
+    buf = torch.full((n + 2,), 0.5, dtype=torch.bfloat16, device="cuda")
+    t = buf[1:-1]
+    t[-1] = 3.0
+    t[(1 << 29) - 1] = -2.0
+    sq = torch.zeros(1, dtype=torch.float64, device="cuda")
+    hl.hl_grad_sq(h, hl.GradList([t]), sq, ws)
+    assert float(sq) == 0.25 * (n - 2) + 9 + 4  # (a multiple of 1/4 below 2^53)
+    norm = math.sqrt(float(sq))
+    hl.hl_grad_clip(h, hl.GradList([t]), sq, float(np.float32(norm / 4)))
+    c = float(np.float32(norm / 4)) / norm
+    for at, v in ((0, 0.5), ((1 << 29) - 1, -2.0), (1 << 29, 0.5), (n - 2, 0.5), (n - 1, 3.0)):
+        assert clipped_ok(torch.tensor([v], dtype=torch.bfloat16, device="cuda"), t[at:at + 1], c)
+    assert int((t == t[0]).sum()) == n - 2 and float(buf[0]) == 0.5 and float(buf[-1]) == 0.5
+
+
+def test_many_launches(h, ws):
+    """More tensors than the sums of eight launches' blocks have room for: added up in between."""
+    m, n = 2300, 150_001
+    flat = torch.ones(m * n, device="cuda")
+    flat[:n] = 2.0
+    flat[-n:] = 3.0
+    ts = [flat[i * n:(i + 1) * n] for i in range(m)]
+    sq, norm = torch.zeros(1, dtype=torch.float64, device="cuda"), torch.zeros(1, device="cuda")
+    grads = hl.GradList(ts)
+    for _ in range(2):
+        hl.hl_grad_sq(h, grads, sq, ws)
+        want = float(n) * (m - 2 + 4 + 9)
+        assert float(sq) == want
+    hl.hl_grad_clip(h, grads, sq, float(np.float32(math.sqrt(want) / 8)), norm)
+    assert abs(float(norm) - math.sqrt(want)) <= 2 * U * float(norm)
+    c = float(np.float32(math.sqrt(want) / 8)) / math.sqrt(want)
+    for i, v in ((0, 2.0), (1, 1.0), (m // 2, 1.0), (m - 1, 3.0)):
+        assert clipped_ok(torch.full((n,), v, device="cuda"), ts[i], c)
+    assert torch.equal(flat[n:-n], flat[n].expand(flat.numel() - 2 * n))
+    assert hl.hl_last_device_error(h) == 0
+
+
 def test_empty_list(h, ws):
     sq, norm = torch.full((1,), 7.0, dtype=torch.float64, device="cuda"), torch.full((1,), 7.0, device="cuda")
     hl.hl_grad_sq(h, hl.GradList([]), sq, ws)

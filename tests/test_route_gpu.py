@@ -371,6 +371,9 @@ def test_refusals(h):
         assert L.hl_route_plan(h.ptr, hl.C.byref(q.struct), p.experts.data_ptr(), None, 0, None) == want, kw
         assert L.hl_route_gather(h.ptr, hl.C.byref(q.struct), 0, 8, x.data_ptr(), 8, rows.data_ptr(), 8, None) == want
     S, X, R = hl.C.byref(r.struct), x.data_ptr(), rows.data_ptr()
+    assert L.hl_route_gather(h.ptr, S, 0, (1 << 20) + 1, X, 1 << 21, R, 1 << 21, None) == 5
+    q = with_field(n_tokens=1 << 28, k=1, n_rows=1 << 29)
+    assert L.hl_route_gather(h.ptr, hl.C.byref(q.struct), 0, 1 << 20, X, 1 << 20, R, 1 << 20, None) == 5
     assert L.hl_route_plan(h.ptr, S, None, None, 0, None) == 1
     assert L.hl_route_plan(h.ptr, None, p.experts.data_ptr(), None, 0, None) == 1
     for args in [(3, 8, X, 8, R, 8), (-1, 8, X, 8, R, 8), (0, 0, X, 8, R, 8), (0, 8, X, 7, R, 8), (0, 8, X, 8, R, 7),
