@@ -117,6 +117,8 @@ class HotPath:
         self.ev_fwdhot = ev()
         self.ev_wb = [ev() for _ in range(self.n_sets)]
         self.out = torch.zeros((max(1, max_bags), w.dim), dtype=torch.float32, device=device)
+        self.norm_parts = torch.zeros(1, dtype=torch.float64, device=device)
+        self.grad_norm = torch.zeros(1, dtype=torch.float32, device=device)  # of the last clipped step
         self.n_hot = 0
 
     def _use(self, p):
@@ -202,7 +204,7 @@ class HotPath:
 
     # ------------------------------------------------------------------ one mini-batch
     def step(self, b: DevBatch, lr: float | None = None, events=None, mode: str = "pipelined", split_fwd=True,
-             untied=False, next=None, handover_kernels=False):
+             untied=False, next=None, handover_kernels=False, max_norm: float | None = None, norm_parts=None):
         """classify -> partition -> remap -> cold gather (non-popular) -> forward of
         both mu-batches -> one coalesced SGD step [-> write-back of the cold rows].
 
@@ -217,7 +219,11 @@ class HotPath:
           the path's kernels hold no waits.
         mode "sequential": the fused calls in order on the current stream;
           `events`: optional list of len(STAGES)+1 torch.cuda.Event recorded
-          around the stages.
+          around the stages.  max_norm: the update is clipped by the step's
+          gradient norm (hl_embbag_bwd_norm, hl_embbag_bwd_clip), which
+          self.grad_norm receives; norm_parts: the norm's parts, a float64
+          tensor whose first entry receives the tables' part and whose others
+          hold the rest of the model's (hl_grad_sq; none by default).
         mode "fwdbwd": as pipelined, but the fetch is awaited before the
           forward/backward section, which `events` (two events) brackets."""
         if mode not in MODES:
@@ -226,8 +232,12 @@ class HotPath:
         B, bps, L = b.n_samples, b.bps, b.n_lookups
         if next is not None and mode != "pipelined":
             raise ValueError("look-ahead needs the native pipelined step")
+        if max_norm is not None and mode != "sequential":
+            raise ValueError("clipping needs every gradient before the first update: mode \"sequential\"")
+        if norm_parts is not None and max_norm is None:
+            raise ValueError("norm_parts without max_norm")
         if mode == "sequential":
-            return self._step_sequential(b, lr, events, split_fwd)
+            return self._step_sequential(b, lr, events, split_fwd, max_norm, norm_parts)
         caller = torch.cuda.current_stream(self.device)
         capturing = torch.cuda.is_current_stream_capturing()
         if mode == "fwdbwd" or capturing:  # the Python rendering of the schedule (a graph keeps no CU mask)
@@ -329,7 +339,7 @@ class HotPath:
             self.step(b, lr=lr, mode="pipelined")
         return g, next(s for s in self._sets if s.codes is self.codes)
 
-    def _step_sequential(self, b, lr, events, split_fwd):
+    def _step_sequential(self, b, lr, events, split_fwd, max_norm=None, norm_parts=None):
         B, bps, L = b.n_samples, b.bps, b.n_lookups
         ev = events
         p = self._next_set()
@@ -369,7 +379,14 @@ class HotPath:
                              None, None, B, self.out)
             mark(6)
         mark(7)
-        if b.dY is not None:
+        if b.dY is not None and max_norm is not None:
+            if split_fwd:
+                hl.hl_embbag_bwd_plan(self.h, self.staging_cap, self.codes, b.bag_ptr, B, bps, L, None, None, B, self.ws)
+            parts = self.norm_parts if norm_parts is None else norm_parts
+            hl.hl_embbag_bwd_norm(self.h, self.staging_cap, B, bps, L, b.dY, parts, self.ws)
+            hl.hl_embbag_bwd_clip(self.h, self.w_hot, self.staging, self.staging_cap, B, bps, L, parts, max_norm, lr,
+                                  self.ws, self.grad_norm)
+        elif b.dY is not None:
             if split_fwd:
                 hl.hl_embbag_bwd_sgd(self.h, self.w_hot, self.staging, self.staging_cap, self.codes, b.bag_ptr, B,
                                      bps, L, None, None, B, b.dY, lr, self.ws)

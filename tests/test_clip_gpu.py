@@ -7,7 +7,9 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2204_05436_amd import hotline as hl
+from paper_2204_05436_amd import configs, hotline as hl, workload as W
+from paper_2204_05436_amd.runner import HotPath, to_device
+from parity_lib import make_table
 
 pytestmark = pytest.mark.gpu
 
@@ -504,6 +506,52 @@ def test_tables_empty():
         assert hl.hl_last_device_error(h) == 0
     finally:
         h.close()
+
+
+@pytest.mark.parametrize("name", ["tiny", "multi-hot"])
+def test_path_step(name):
+    """The path's step with a bound on the norm: far above it bit for bit the plain step, below it the plain step with
+    the scaled learning rate; a dense part counts in the norm."""
+    w = configs.scaled(configs.WORKLOADS[name], batch=200, row_scale=0.02, name=name + "-clip")
+    rows = W.table_rows(w)
+    prof = [W.make_batch(w, rows, i) for i in range(3)]
+    mb = W.make_batch(w, rows, 3)
+    table = make_table(w, int(rows.sum(dtype=np.int64)))
+    hp = HotPath(w, rows, table, max(x.n_lookups for x in prof + [mb]), w.batch)
+    try:
+        hp.learn([to_device(p, "cuda") for p in prof])
+        b = to_device(mb, "cuda", W.make_dy(w, 3, mb.n_bags))
+        start = hp.w_hot.clone()
+
+        def step(**kw):
+            hp.w_hot.copy_(start)
+            hp.step(b, mode="sequential", **kw)
+            return hp.w_hot.clone(), hp.staging[:int(hp.n_cold.item())].clone()
+
+        same = lambda x, y: all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(x, y))
+        for split in (True, False):
+            assert same(step(split_fwd=split, max_norm=math.inf), step(split_fwd=split))
+            norm = math.sqrt(float(hp.norm_parts))
+            assert abs(float(hp.grad_norm) - norm) <= 2 * U * norm
+            m = float(np.float32(norm / 5))
+            parts = torch.tensor([0.0, 3 * norm * norm], dtype=torch.float64, device="cuda")  # (the norm is twice this)
+            for p, full in ((None, norm), (parts, None)):
+                got = step(split_fwd=split, max_norm=m, norm_parts=p)
+                if p is not None:
+                    full = math.sqrt(float(parts[0]) + float(parts[1]))
+                    assert abs(full - 2 * norm) <= 1e-9 * norm
+                lr = float(np.float32(w.lr) * np.float32(m / full))
+                assert same(got, step(split_fwd=split, lr=lr))
+                assert not same(got, step(split_fwd=split))
+        for kw in (dict(mode="pipelined"), dict(mode="fwdbwd")):
+            with pytest.raises(ValueError):
+                hp.step(b, max_norm=1.0, **kw)
+        with pytest.raises(ValueError):
+            hp.step(b, mode="sequential", norm_parts=parts)
+        assert hp.device_error() == 0
+    finally:
+        hp.close()
+        table.close()
 
 
 def test_stream_and_graphs(h, ws):
