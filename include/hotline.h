@@ -516,9 +516,9 @@ hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int32_t n_grads
  * keeps the sums in the workspace and writes the sum of their squares, over every
  * row of the plan, to *sq (device); it reads no embedding row.
  * hl_embbag_bwd_clip then updates row(c) <- round_storage(row(c) - lr * c * G_c)
- * from the kept sums (c as above; with c = 0 no row is written), bit for bit
- * hl_embbag_bwd_apply with lr * c in place of lr (one fp32 product); norm_out as
- * in hl_grad_clip.  Arguments as hl_embbag_bwd_apply's.  The norm needs a plan
+ * from the kept sums (c as above; with c = 0 no row is written): for rows at
+ * 16-byte addresses and c >= 2^-100 bit for bit hl_embbag_bwd_apply with lr * c in
+ * place of lr (one fp32 product); norm_out as in hl_grad_clip.  Arguments as hl_embbag_bwd_apply's.  The norm needs a plan
  * (made by hl_embbag_bwd_plan or hl_embbag_fwd_plan), the clipped update the norm
  * on the same plan with no other call on that workspace in between, else
  * HL_ERR_INVALID_ARG; it may be applied more than once (each a step with the same
