@@ -431,7 +431,8 @@ hl_status hl_debug_ballot_ranks(hl_handle* h, int32_t on);
  * Limits (HL_ERR_UNSUPPORTED): n_experts <= 1024, n_tokens*k <= 2^30, rows < 2^31.
  * HL_ERR_CAPACITY: n_rows or the workspace (hl_route_workspace_bytes; any
  * contents, NULL allowed where the call needs none: up to 4096 assignments) is
- * too small.  A workspace of other calls may serve (a plan that it held is lost).  The handle's device must be the current one. */
+ * too small.  A workspace of other calls may serve (a plan that it held is lost).
+ * The handle's device must be the current one. */
 typedef struct hl_route {
   int64_t n_tokens;
   int32_t k;
@@ -515,10 +516,11 @@ hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int32_t n_grads
  * hl_embbag_bwd_norm reduces dY over each group (G_c as in hl_embbag_bwd_sgd),
  * keeps the sums in the workspace and writes the sum of their squares, over every
  * row of the plan, to *sq (device); it reads no embedding row.
- * hl_embbag_bwd_clip then updates row(c) <- round_storage(row(c) - lr * c * G_c)
- * from the kept sums (c as above; with c = 0 no row is written): for rows at
- * 16-byte addresses and c >= 2^-100 bit for bit hl_embbag_bwd_apply with lr * c in
- * place of lr (one fp32 product); norm_out as in hl_grad_clip.  Arguments as hl_embbag_bwd_apply's.  The norm needs a plan
+ * hl_embbag_bwd_clip then updates row(c) <- round_storage(row(c) - lr * f * G_c)
+ * from the kept sums, f being the factor c of the clipping above (with f = 0 no row
+ * is written): for rows at 16-byte addresses and f >= 2^-100 bit for bit
+ * hl_embbag_bwd_apply with lr * f in place of lr (one fp32 product).  norm_out as in
+ * hl_grad_clip, the other arguments as hl_embbag_bwd_apply's.  The norm needs a plan
  * (made by hl_embbag_bwd_plan or hl_embbag_fwd_plan), the clipped update the norm
  * on the same plan with no other call on that workspace in between, else
  * HL_ERR_INVALID_ARG; it may be applied more than once (each a step with the same
