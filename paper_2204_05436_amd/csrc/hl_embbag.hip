@@ -170,10 +170,13 @@ static size_t bw_bytes(const hl_handle* h, int64_t n, int64_t bags, bool compact
   return compact ? hl_bwd_ws_bytes_compact(h, n, bags) : hl_bwd_ws_bytes(h, n, bags);
 }
 
+// The selected samples: without a list the first n_max (phase 0), else the listed
+// ones (phase 1, after phase 0 has cleared the mask).
 __global__ void bw_mask(uint8_t* mask, int32_t n_samples, const int32_t* __restrict__ ids, const int32_t* n_dev,
                         int32_t n_max, int phase) {
   if (phase == 0) {
-    for (int32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < n_samples; i += gridDim.x * blockDim.x) mask[i] = 0;
+    for (int32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < n_samples; i += gridDim.x * blockDim.x)
+      mask[i] = !ids && i < n_max;
   } else {
     const int32_t n = eb_nsel(ids, n_dev, n_max);
     for (int32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
@@ -1178,7 +1181,8 @@ hl_status hl_embbag_bwd_plan_signal(hl_handle* h, int32_t stg_rows, int32_t* cod
                                     const hl_cg_fused* cf, bool compact) {
   *sent = false;
   if (compact && cf && cf->table) return HL_ERR_INVALID_ARG;  // the fused plan's state follows the full layout
-  if (cf && cf->table && sample_ids) return HL_ERR_INVALID_ARG;  // the fused plan selects every sample
+  const bool some = sample_ids || n_sel_max < n_samples;     // (a selection, not the whole mini-batch)
+  if (cf && cf->table && some) return HL_ERR_INVALID_ARG;    // the fused plan selects every sample
   hl_status st = check_common(h, codes, bag_ptr, n_samples, bps, n_lookups, sample_ids, n_sel_max, stg_rows);
   if (st != HL_OK) return st;
   if (!workspace) return HL_ERR_INVALID_ARG;
@@ -1195,11 +1199,12 @@ hl_status hl_embbag_bwd_plan_signal(hl_handle* h, int32_t stg_rows, int32_t* cod
   bw_ws ws;
   bw_carve(c, ws, (uint32_t)n_lookups, n_bags, h->dim, compact);
   const uint8_t* mask = nullptr;
-  if (sample_ids) {
+  if (some) {
     uint32_t gb = hl_div_up(n_samples, 256);
     if (gb > 4096) gb = 4096;
     HL_KERNEL(h, s, "bw_mask", bw_mask, dim3(gb), dim3(256), 0, s, ws.mask, n_samples, sample_ids, n_sel_dev, n_sel_max, 0);
-    HL_KERNEL(h, s, "bw_mask", bw_mask, dim3(gb), dim3(256), 0, s, ws.mask, n_samples, sample_ids, n_sel_dev, n_sel_max, 1);
+    if (sample_ids)
+      HL_KERNEL(h, s, "bw_mask", bw_mask, dim3(gb), dim3(256), 0, s, ws.mask, n_samples, sample_ids, n_sel_dev, n_sel_max, 1);
     mask = ws.mask;
   }
   uint32_t *sk, *sv;
