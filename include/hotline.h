@@ -346,7 +346,8 @@ hl_status hl_embbag_bwd_sgd_noalloc(hl_handle* h, void* w_hot, void* staging, in
  * staging_rows, n_samples, bags_per_sample and n_lookups and the same
  * workspace, with no other call on that workspace in between; otherwise it
  * returns HL_ERR_INVALID_ARG and changes nothing.  Applying one plan twice is
- * two SGD steps with the same grouping. */
+ * two SGD steps with the same grouping; applying a plan that selects no sample
+ * changes no row. */
 hl_status hl_embbag_bwd_plan(hl_handle* h, int32_t staging_rows, const int32_t* codes,
                              const int32_t* bag_ptr, int32_t n_samples, int32_t bags_per_sample,
                              int64_t n_lookups, const int32_t* sample_ids, const int32_t* n_sel_dev,

@@ -1190,8 +1190,9 @@ hl_status hl_embbag_bwd_plan_signal(hl_handle* h, int32_t stg_rows, int32_t* cod
   if (ws_bytes < bw_bytes(h, n_lookups, n_bags, compact)) return HL_ERR_CAPACITY;
   hl_ws_note(h, workspace, HL_WSK_OTHER);
   if (n_samples == 0 || n_lookups == 0 || n_sel_max == 0) {
-    hl_ws_note(h, workspace, HL_WSK_BWD_PLAN, 0, n_bags, stg_rows);
+    hl_ws_note(h, workspace, HL_WSK_BWD_PLAN, n_lookups, n_bags, stg_rows);
     hl_ws_find(h, workspace)->compact = compact;
+    hl_ws_find(h, workspace)->none = 1;
     return HL_OK;
   }
   hipStream_t s = (hipStream_t)stream;
@@ -1386,7 +1387,7 @@ hl_status hl_embbag_bwd_apply_any(hl_handle* h, void* w_hot, void* staging, int3
     return HL_ERR_INVALID_ARG;  // no matching plan is held by this workspace
   if (part == 2 && rec->part1 != 1) return HL_ERR_INVALID_ARG;  // the first half has not run on this plan
   if (part != 0 && rec->compact) return HL_ERR_INVALID_ARG;      // no room for the staging-row sums
-  if (n_lookups == 0 || n_samples == 0) {
+  if (rec->none) {
     if (part == 1 || part == 3) rec->part1 = part == 1 ? 1 : 3;
     return HL_OK;
   }
@@ -1461,7 +1462,7 @@ extern "C" hl_status hl_embbag_bwd_norm(hl_handle* h, int32_t stg_rows, int32_t 
   if (st != HL_OK) return st;
   hipStream_t s = (hipStream_t)stream;
   const int vec = eb_pick_vec(h->dim, h->dtype == HL_F32 ? 4 : 2, {dY});
-  if (rec->n == 0 || n_samples == 0) {
+  if (rec->none) {
     st = hl_fill32((uint32_t*)sq, 2, 0, s);
   } else {
     if (!dY) return HL_ERR_INVALID_ARG;
@@ -1495,7 +1496,7 @@ extern "C" hl_status hl_embbag_bwd_clip(hl_handle* h, void* w_hot, void* staging
   hl_status st = norm_setup(h, stg_rows, n_samples, bps, n_lookups, workspace, ws_bytes, &rec, &ws, &sk, &sv);
   if (st != HL_OK) return st;
   if (rec->part1 != 4) return HL_ERR_INVALID_ARG;  // the norm has not run on this plan
-  const bool none = rec->n == 0 || n_samples == 0;
+  const bool none = rec->none;
   if (!none && ((h->n_hot && !w_hot) || (stg_rows && !staging))) return HL_ERR_INVALID_ARG;
   if (none && !norm_out) return HL_OK;
   const int vec = eb_pick_vec(h->dim, h->dtype == HL_F32 ? 4 : 2, {w_hot, staging});
@@ -1568,6 +1569,7 @@ hl_status hl_embbag_finish_cold(hl_handle* h, void* w_hot, void* staging, int32_
     return HL_ERR_INVALID_ARG;  // the grouping and apply part 3 must be in this workspace
   rec->part1 = 0;  // the plan is used up: no part 2 or second finish on it
   if (n_lookups == 0 || n_samples == 0) return HL_OK;
+  if (rec->none) return HL_ERR_INVALID_ARG;  // the plan must select every sample
   if (ws_bytes < bw_bytes(h, n_lookups, n_bags, rec->compact)) return HL_ERR_CAPACITY;
   hl_carver c = hl_carver::after_header(workspace, ws_bytes);
   bw_ws ws;
@@ -1650,13 +1652,17 @@ extern "C" hl_status hl_embbag_bwd_grouping(hl_handle* h, int32_t stg_rows, int3
   hl_ws_rec* rec = hl_ws_find(h, workspace);
   if (!rec || rec->n != n_lookups || rec->bags != n_bags || rec->stg != stg_rows) return HL_ERR_INVALID_ARG;
   if (n_lookups == 0) return HL_OK;
+  hipStream_t s = (hipStream_t)stream;
+  if (rec->none) {  // every lookup was skipped
+    hl_status st = hl_fill32(keys_out, (uint64_t)n_lookups, EB_SENT, s);
+    return st != HL_OK ? st : hl_fill32(bags_out, (uint64_t)n_lookups, 0, s);
+  }
   if (ws_bytes < bw_bytes(h, n_lookups, n_bags, rec->compact)) return HL_ERR_CAPACITY;
   hl_carver c = hl_carver::after_header(const_cast<void*>(workspace), ws_bytes);
   bw_ws ws;
   bw_carve(c, ws, (uint32_t)n_lookups, n_bags, h->dim, rec->compact);
   uint32_t *sk, *sv;
   hl_sort_result(ws.sort, bw_key_bits(h, stg_rows), &sk, &sv);
-  hipStream_t s = (hipStream_t)stream;
   if (hipMemcpyAsync(keys_out, sk, (size_t)n_lookups * 4, hipMemcpyDeviceToDevice, s) != hipSuccess ||
       hipMemcpyAsync(bags_out, sv, (size_t)n_lookups * 4, hipMemcpyDeviceToDevice, s) != hipSuccess)
     return HL_ERR_HIP;

@@ -47,6 +47,7 @@ struct hl_ws_rec {
   int vec;             // the row vector width that half used (its tile layout depends on it)
   int compact;         // the plan used the layout without the staging-row sums (whole applies only)
   uint32_t n_hot;      // the hot set's size, which the keys depend on
+  int none;            // the plan selects no lookup: nothing was grouped
 };
 struct hl_handle {
   int device;
@@ -107,7 +108,7 @@ static inline void hl_ws_note(hl_handle* h, const void* ws, int kind, int64_t n 
     r = &h->ws_rec[h->ws_next];
     h->ws_next = (h->ws_next + 1) % 4;
   }
-  *r = {ws, n, bags, stg, 0, 0, 0, h->n_hot};
+  *r = {ws, n, bags, stg, 0, 0, 0, h->n_hot, 0};
 }
 static inline hl_ws_rec* hl_ws_find(hl_handle* h, const void* ws) {
   for (auto& r : h->ws_rec)

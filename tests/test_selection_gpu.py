@@ -1,6 +1,6 @@
 """The backward's calls over the first samples of a mini-batch (no list: samples 0 .. n_sel_max - 1) against plain sums
 in 64 bits, and bit for bit against the same samples as a list: the one-call update, with and without a workspace, the
-plan with the update, and the plan with the norm and the clipped update."""
+plan with the update, and the plan with the norm and the clipped update; and over no sample at all."""
 import math
 
 import numpy as np
@@ -76,6 +76,42 @@ def test_first_samples(dt, dim, bag, n_sel):
         m = int(take.sum())
         assert np.array_equal(keys[:m].cpu().numpy(), t.row[take][by_row]) and bool((keys[m:] == -1).all())
         assert np.array_equal(bags[:m].cpu().numpy(), t.bag[take][by_row])
+        assert hl.hl_last_device_error(t.h) == 0
+    finally:
+        t.h.close()
+
+
+@pytest.mark.parametrize("dt,dim,bag", [("f32", 64, 0.0), ("bf16", 40, 2.5)])
+@pytest.mark.parametrize("how", ["none", "no list", "device count"])
+def test_no_samples(dt, dim, bag, how):
+    """A selection of no sample of a mini-batch with lookups: no row changes, and the norm is zero."""
+    t = Tables(3, 90, dim, dt, 50, bag, seed=8)
+    try:
+        i32 = dict(dtype=torch.int32, device="cuda")
+        ids = None if how == "none" else torch.zeros(4, **i32)
+        n_sel, n_dev = (4, torch.zeros(1, **i32)) if how == "device count" else (0, None)
+        w = t.w.clone()
+        for form in FORMS:
+            t.sq.fill_(7.0)
+            t.norm.fill_(7.0)
+            form(t, w, ids, n_sel, n_dev)
+            assert torch.equal(w, t.w), form.__name__
+        assert float(t.sq) == 0 and float(t.norm) == 0
+        plan(t, ids, n_sel, n_dev)
+        for part in (1, 2):
+            hl.hl_embbag_bwd_apply_part(t.h, w[:t.n_hot], w[t.n_hot:], *t.shape(), t.dY, LR, part, t.ws)
+        keys, bags = (torch.zeros(t.L, **i32) for _ in range(2))
+        hl.hl_embbag_bwd_grouping(t.h, *t.shape(), t.ws, keys, bags)
+        assert bool((keys == -1).all()) and torch.equal(w, t.w)
+        # other sizes than the plan's are refused as ever
+        for f in (lambda: hl.hl_embbag_bwd_apply(t.h, w[:t.n_hot], w[t.n_hot:], t.n_stg, t.B, t.T, t.L - 1, t.dY, LR, t.ws),
+                  lambda: hl.hl_embbag_bwd_norm(t.h, t.n_stg, t.B, t.T, t.L - 1, t.dY, t.sq, t.ws)):
+            with pytest.raises(hl.HotlineError):
+                f()
+        # the next plan on this workspace groups as ever
+        G, _, n = t.sums()
+        apply(t, w, None, t.B)
+        assert not torch.equal(w, t.w) and torch.equal(w[n == 0], t.w[n == 0])
         assert hl.hl_last_device_error(t.h) == 0
     finally:
         t.h.close()
