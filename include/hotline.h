@@ -519,9 +519,12 @@ hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int32_t n_grads
  * row of the plan, to *sq (device); it reads no embedding row.
  * hl_embbag_bwd_clip then updates row(c) <- round_storage(row(c) - lr * f * G_c)
  * from the kept sums, f being the factor c of the clipping above (with f = 0 no row
- * is written): for rows at 16-byte addresses and f >= 2^-100 bit for bit
- * hl_embbag_bwd_apply with lr * f in place of lr (one fp32 product).  norm_out as in
- * hl_grad_clip, the other arguments as hl_embbag_bwd_apply's.  The norm needs a plan
+ * is written): for f >= 2^-100 bit for bit hl_embbag_bwd_apply with lr * f in place
+ * of lr (one fp32 product), if w_hot and staging are multiples of 16 bytes, for bf16
+ * rows of a multiple of 8 elements of 32.  (At other addresses the apply reads
+ * narrower pieces than the norm, which sees dY alone, and may add a long run's
+ * gradients in another order.)  norm_out as in hl_grad_clip, the other arguments as
+ * hl_embbag_bwd_apply's.  The norm needs a plan
  * (made by hl_embbag_bwd_plan or hl_embbag_fwd_plan), the clipped update the norm
  * on the same plan with no other call on that workspace in between, else
  * HL_ERR_INVALID_ARG; it may be applied more than once (each a step with the same
