@@ -526,9 +526,10 @@ hl_status hl_grad_clip(const hl_handle* h, const hl_grad* grads, int32_t n_grads
  * gradients in another order.)  norm_out as in hl_grad_clip, the other arguments as
  * hl_embbag_bwd_apply's.  The norm needs a plan
  * (made by hl_embbag_bwd_plan or hl_embbag_fwd_plan), the clipped update the norm
- * on the same plan with no other call on that workspace in between, else
- * HL_ERR_INVALID_ARG; it may be applied more than once (each a step with the same
- * sums). */
+ * on the same plan, else HL_ERR_INVALID_ARG; a call in between that writes that
+ * workspace's buffers loses the sums.  hl_embbag_bwd_apply and
+ * hl_embbag_bwd_grouping keep them, and the clipped update may be applied more
+ * than once (each a step with the same sums). */
 hl_status hl_embbag_bwd_norm(hl_handle* h, int32_t staging_rows, int32_t n_samples, int32_t bags_per_sample,
                              int64_t n_lookups, const float* dY, double* sq, void* workspace, size_t ws_bytes,
                              hl_stream stream);

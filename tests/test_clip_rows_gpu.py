@@ -1,6 +1,6 @@
 """The clipped table update against the plain one where runs of equal rows span many tiles and their sums cancel to
 rounding errors, so that another order of the additions shows: bit for bit where both calls take as many elements per
-lane, within the bound of an fp32 sum where they do not."""
+lane, within the bound of an fp32 sum where they do not.  And which calls may come between the norm and the update."""
 import math
 
 import numpy as np
@@ -57,6 +57,46 @@ def test_cancelling_runs(dt, dim, n_hot, same):
             t.clip(a, m, 0.25)
             t.apply(b, float(np.float32(0.25) * c))
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        assert hl.hl_last_device_error(t.h) == 0
+    finally:
+        t.h.close()
+
+
+def test_calls_in_between():
+    """The plain update and the grouping keep the norm's sums; calls that write the workspace's buffers lose them."""
+    t = Tables(3, 200, 16, "f32", 300, 2.0, seed=4)
+    try:
+        i32 = dict(dtype=torch.int32, device="cuda")
+        w, other = t.w.clone(), t.w.clone()
+        keys, bags = torch.zeros(t.L, **i32), torch.zeros(t.L, **i32)
+        t.plan()
+        t.norm_()
+        t.clip(w, 1.0, 0.5)
+        keep = lambda: t.apply(other, 0.1), lambda: hl.hl_embbag_bwd_grouping(t.h, *t.shape(), t.ws, keys, bags)
+        for f in keep:
+            f()
+            again = t.w.clone()
+            t.clip(again, 1.0, 0.5)
+            assert torch.equal(again, w)
+        assert not torch.equal(w, t.w)
+        k, E = 8, 16
+        route = hl.Route(4096, k, E, torch.zeros(E, **i32), torch.zeros(E + 1, **i32), torch.zeros(4096 * k, **i32))
+        experts = torch.zeros(4096 * k, **i32)
+        ws = torch.zeros(max(t.ws.numel(), hl.hl_grad_workspace_bytes(), hl.hl_route_workspace_bytes(4096, k, E)),
+                         dtype=torch.uint8, device="cuda")
+        t.ws = ws
+        lose = [t.plan, lambda: hl.hl_route_plan(t.h, route, experts, ws),
+                lambda: hl.hl_grad_sq(t.h, hl.GradList([other]), torch.zeros(1, dtype=torch.float64, device="cuda"), ws),
+                lambda: hl.hl_embbag_bwd_sgd(t.h, other[:t.n_hot], other[t.n_hot:], t.n_stg, t.codes, t.ptr_d, t.B, t.T,
+                                             t.L, None, None, t.B, t.dY, 0.1, ws)]
+        for f in lose:
+            t.plan()
+            t.norm_()
+            f()
+            with pytest.raises(hl.HotlineError) as e:
+                t.clip(w, 1.0, 0.5)
+            assert e.value.status == 1
+        torch.cuda.synchronize()
         assert hl.hl_last_device_error(t.h) == 0
     finally:
         t.h.close()
