@@ -87,10 +87,9 @@ def kernel_bytes(name, st, alone=False):
         "gt_sort": 12 * L,
         # hot half of the forward over every bag: codes, offsets, each referenced row once, outputs
         "eb_fwd_hot": 4 * L + 4 * (nb + 1) + (U - C) * R + nb * O,
-        # cold half: tail keys and bags, offsets, staging rows, outputs read and written
-        "eb_fwd_tail": 8 * Lc + 8 * Lc + C * R + 2 * Lc * O,
-        # the same with the reduction's spanning segments (their partial sums are
-        # workspace, not algorithmic bytes)
+        # cold half: tail keys and bags, offsets, staging rows, outputs read and
+        # written (the reduction's spanning segments beside it: their partial sums
+        # are workspace, not algorithmic bytes)
         "eb_tail_r2": 8 * Lc + 8 * Lc + C * R + 2 * Lc * O,
         # the cold half bag by bag (multi-hot): codes and offsets of every bag,
         # staging rows, outputs read and written
@@ -432,7 +431,7 @@ def main():
 
     # the embedding forward and backward: their kernels' time per step (the
     # grouping included), against the algorithmic bytes of both passes
-    fb_kernels = ("eb_fwd", "eb_fwd_gt", "eb_fwd_srt", "eb_fwd_hot", "eb_fwd_tail", "eb_tail_r2", "eb_bags_r2", "bw_prep",
+    fb_kernels = ("eb_fwd", "eb_fwd_gt", "eb_fwd_srt", "eb_fwd_hot", "eb_tail_r2", "eb_bags_r2", "bw_prep",
                   "srt_count", "srt_pass", "gt_prep", "gt_sort", "bw_reduce1", "bw_reduce2", "bw_cold")
     t_fb = sum(kernels[n]["ms_per_step"] for n in fb_kernels if n in kernels)
     t_fb_alone = sum(kernels_alone[n]["ms_per_step"] for n in fb_kernels if n in kernels_alone)
@@ -632,7 +631,7 @@ def main():
 
 
 # the main stream's kernels of a planned step: the forwards and the backward
-MAIN_KERNELS = ("eb_fwd_hot", "eb_fwd_cold", "eb_fwd_tail", "eb_tail_r2", "eb_bags_r2", "bw_reduce1", "bw_reduce2",
+MAIN_KERNELS = ("eb_fwd_hot", "eb_fwd_cold", "eb_tail_r2", "eb_bags_r2", "bw_reduce1", "bw_reduce2",
                 "bw_cold")
 
 

@@ -863,8 +863,8 @@ bw_cold(const uint32_t* __restrict__ keys, uint32_t n, eb_geom g, void* stg, uin
 // the forward's cold half over the non-popular mu-batch.  A group of lanes
 // takes FT pairs at once.
 #define FT 4
-// (block bid of nblk, WAVES waves per block)
-template <int VEC, bool BF, int WAVES>
+// (block bid of nblk, RB_WAVES waves per block)
+template <int VEC, bool BF>
 __device__ __forceinline__ void eb_tail_body(uint32_t bid, uint32_t nblk, const uint32_t* __restrict__ keys,
                                              const uint32_t* __restrict__ vals, uint32_t n,
                                              const uint32_t* __restrict__ bnd, eb_geom g, const void* stg_,
@@ -880,8 +880,8 @@ __device__ __forceinline__ void eb_tail_body(uint32_t bid, uint32_t nblk, const 
   const bool cact = colv < g.vpr;
   const int64_t col = (int64_t)colv * VEC;
   const uint32_t b0 = min(*bnd, n);
-  const uint64_t stride = (uint64_t)nblk * WAVES * g.NG * FT;
-  for (uint64_t p0 = b0 + ((uint64_t)(bid * WAVES + w) * g.NG + gi) * FT; p0 < n; p0 += stride) {
+  const uint64_t stride = (uint64_t)nblk * RB_WAVES * g.NG * FT;
+  for (uint64_t p0 = b0 + ((uint64_t)(bid * RB_WAVES + w) * g.NG + gi) * FT; p0 < n; p0 += stride) {
     uint32_t key[FT], bag[FT];
     bool take[FT];
 #pragma unroll
@@ -966,16 +966,6 @@ __device__ __forceinline__ void eb_tail_body(uint32_t bid, uint32_t nblk, const 
   }
 }
 
-template <int VEC, bool BF>
-__global__ void __launch_bounds__(256)
-eb_fwd_tail(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ vals, uint32_t n,
-            const uint32_t* __restrict__ bnd, eb_geom g, const void* stg_, int32_t stg_rows, uint32_t n_hot,
-            uint32_t k_cap, const int32_t* __restrict__ codes, const int32_t* __restrict__ bag_ptr,
-            float* __restrict__ out, uint32_t* err) {
-  eb_tail_body<VEC, BF, 4>(blockIdx.x, gridDim.x, keys, vals, n, bnd, g, stg_, stg_rows, n_hot, k_cap, codes, bag_ptr,
-                           out, err);
-}
-
 // The cold half of the forward and the backward's segments that span tiles
 // (bw_reduce2, split form) in one launch: the first blocks take the
 // segments, the others the sorted tail.  They share no data (the segments
@@ -995,8 +985,8 @@ eb_tail_r2(uint32_t n_tiles, void* w_hot, uint32_t n_hot, float lr, const float*
                                        gc_rows, nullptr);
     return;
   }
-  eb_tail_body<VEC, BF, RB_WAVES>(blockIdx.x - r2, gridDim.x - r2, keys, vals, n, bnd, g, stg, stg_rows,
-                                  n_hot, k_cap, codes, bag_ptr, out, err);
+  eb_tail_body<VEC, BF>(blockIdx.x - r2, gridDim.x - r2, keys, vals, n, bnd, g, stg, stg_rows, n_hot, k_cap, codes,
+                        bag_ptr, out, err);
 }
 
 // The same launch for bags of several lookups (multi-hot), where nearly every
@@ -1513,43 +1503,6 @@ extern "C" hl_status hl_embbag_bwd_clip(hl_handle* h, void* w_hot, void* staging
   else if (vec == 2) { if (bf) CLIP(2, true); else CLIP(2, false); }
   else { if (bf) CLIP(1, true); else CLIP(1, false); }
 #undef CLIP
-  HL_LAUNCHED();
-  return HL_OK;
-}
-
-hl_status hl_embbag_fwd_cold_sorted(hl_handle* h, const void* staging, int32_t stg_rows, const int32_t* codes,
-                                    const int32_t* bag_ptr, int32_t n_samples, int32_t bps, int64_t n_lookups,
-                                    float* out, void* workspace, size_t ws_bytes, hl_stream stream) {
-  hl_status st = check_common(h, codes, bag_ptr, n_samples, bps, n_lookups, nullptr, n_samples, stg_rows);
-  if (st != HL_OK) return st;
-  if (!workspace || !out || (stg_rows && !staging)) return HL_ERR_INVALID_ARG;
-  const int64_t n_bags = (int64_t)n_samples * bps;
-  hl_ws_rec* rec = hl_ws_find(h, workspace);
-  if (!rec || rec->n != n_lookups || rec->bags != n_bags || rec->stg != stg_rows || !rec->part1)
-    return HL_ERR_INVALID_ARG;  // the grouping and the first apply half must be in this workspace
-  if (n_lookups == 0 || n_samples == 0) return HL_OK;
-  if (ws_bytes < bw_bytes(h, n_lookups, n_bags, rec->compact)) return HL_ERR_CAPACITY;
-  hl_carver c = hl_carver::after_header(workspace, ws_bytes);
-  bw_ws ws;
-  bw_carve(c, ws, (uint32_t)n_lookups, n_bags, h->dim, rec->compact);
-  uint32_t *sk, *sv;
-  hl_sort_result(ws.sort, bw_key_bits(h, stg_rows), &sk, &sv);
-  const size_t es = h->dtype == HL_F32 ? 4 : 2;
-  const int vec = eb_pick_vec(h->dim, es, {staging, out});
-  eb_geom g = eb_make_geom(h->dim, vec);
-  const uint32_t n = (uint32_t)n_lookups;
-  uint32_t b = hl_div_up(n, 4 * g.NG * FT);
-  if (b > 512) b = 512;
-  hipStream_t s = (hipStream_t)stream;
-  const bool bf = h->dtype == HL_BF16;
-#define TAIL(V, B)                                                                                                  \
-  HL_KERNEL(h, s, "eb_fwd_tail", (eb_fwd_tail<V, B>), dim3(b, g.cchunks), dim3(256), 0, s, sk, sv, n, ws.bnd, g, \
-            staging, stg_rows, h->n_hot, h->k_cap, codes, bag_ptr, out, h->d_err)
-  if (vec == 8) TAIL(8, true);  // (bf16 only)
-  else if (vec == 4) { if (bf) TAIL(4, true); else TAIL(4, false); }
-  else if (vec == 2) { if (bf) TAIL(2, true); else TAIL(2, false); }
-  else { if (bf) TAIL(1, true); else TAIL(1, false); }
-#undef TAIL
   HL_LAUNCHED();
   return HL_OK;
 }

@@ -225,22 +225,16 @@ struct hl_carver {
   }
 };
 
-// The cold half of the forward (hl_embbag_fwd_part 2 over the non-popular
-// mu-batch) read from the backward's grouping held in `workspace`: the same
-// sums, over the cold lookups only.  Needs a plan over every sample and the
-// first apply half (which marks where the cold keys start) on that workspace.
-hl_status hl_embbag_fwd_cold_sorted(hl_handle* h, const void* staging, int32_t stg_rows, const int32_t* codes,
-                                    const int32_t* bag_ptr, int32_t n_samples, int32_t bps, int64_t n_lookups,
-                                    float* out, void* workspace, size_t ws_bytes, hl_stream stream);
-
 // hl_embbag_bwd_apply_part with one more part: 3, the first half without the
 // segments that span tiles, which hl_embbag_finish_cold then completes.
 hl_status hl_embbag_bwd_apply_any(hl_handle* h, void* w_hot, void* staging, int32_t stg_rows, int32_t n_samples,
                                   int32_t bps, int64_t n_lookups, const float* dY, float lr, int32_t part,
                                   void* workspace, size_t ws_bytes, hl_stream stream);
-// After part 3, once the staging rows are fetched: the cold half of the
-// forward (as hl_embbag_fwd_cold_sorted) with part 3's spanning segments in one
-// launch, then the staging-row updates (as part 2).
+// After part 3 of a plan over every sample, once the staging rows are fetched:
+// the cold half of the forward (hl_embbag_fwd_part 2 over the non-popular
+// mu-batch) read from the backward's grouping, the same sums over the cold
+// lookups only, with part 3's spanning segments in one launch, then the
+// staging-row updates (as part 2).
 hl_status hl_embbag_finish_cold(hl_handle* h, void* w_hot, void* staging, int32_t stg_rows, const int32_t* codes,
                                 const int32_t* bag_ptr, int32_t n_samples, int32_t bps, int64_t n_lookups, float lr,
                                 float* out, void* workspace, size_t ws_bytes, hl_stream stream);
