@@ -232,9 +232,44 @@ def _check_plain(x, dtype, n, what):
         raise ValueError(f"{what}: {n} contiguous {dtype} elements wanted, got {x.dtype} {tuple(x.shape)}")
 
 
+def _gpu_of(tensors):
+    """The GPU that holds the tensors (None and plain addresses aside).  None: any GPU reaches them (pinned host memory,
+    no elements).  -1: no GPU reaches all of them."""
+    gpu = None
+    for x in tensors:
+        if x is None or isinstance(x, int):
+            continue
+        g = x.get_device()
+        if g < 0:
+            if x.numel() and not x.is_pinned():
+                return -1
+        elif gpu is None or gpu == g:
+            gpu = g
+        else:
+            return -1
+    return gpu
+
+
+def _check_gpu(h, what, *tensors):
+    """Every tensor is where the handle's kernels reach it: an address that they do not reach faults the GPU."""
+    gpu = h.device
+    for x in tensors:
+        if x is None or isinstance(x, int) or x.get_device() == gpu or _gpu_of((x,)) is None:
+            continue
+        raise ValueError(f"{what}: tensors on the handle's GPU wanted (cuda:{gpu}), got one on {x.device}")
+
+
+def _check_held(h, held, what):
+    """As _check_gpu, for a Route or a GradList, which looked at its tensors when it was made."""
+    if held.gpu is not None and held.gpu != h.device:
+        raise ValueError(f"{what}: its tensors on the handle's GPU wanted (cuda:{h.device})")
+
+
 class Handle:
-    def __init__(self, ptr):
-        self.ptr = ptr
+    """device: the GPU that was the current one at its creation; dim: elements of a row."""
+
+    def __init__(self, ptr, device=0, dim=0):
+        self.ptr, self.device, self.dim = ptr, device, dim
         _track(("handle", ptr), self.close)
 
     @property
@@ -265,7 +300,8 @@ def hl_create(rows_per_table, dim, dtype, k_cap):
     h = P()
     dt = HL_F32 if dtype in ("f32", HL_F32) else HL_BF16
     _ck("hl_create", lib().hl_create(C.byref(h), len(rows), rows.ctypes.data, int(dim), dt, int(k_cap)))
-    return Handle(h.value)
+    import torch
+    return Handle(h.value, torch.cuda.current_device(), int(dim))
 
 
 def hl_destroy(h):
@@ -493,6 +529,9 @@ def hl_embbag_bwd_grouping(h, staging_rows, n_samples, bags_per_sample, n_lookup
 def hl_embbag_bwd_norm(h, staging_rows, n_samples, bags_per_sample, n_lookups, dY, sq, ws, stream=None):
     """sq: a float64 tensor, its first entry written."""
     _check_plain(sq, "float64", 1, "sq")
+    if dY is not None and not isinstance(dY, int):
+        _check_plain(dY, "float32", n_samples * bags_per_sample * h.dim, "dY")
+    _check_gpu(h, "hl_embbag_bwd_norm", dY, sq, ws)
     _ck("hl_embbag_bwd_norm", lib().hl_embbag_bwd_norm(
         h.ptr, int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(dY), _p(sq), _p(ws),
         _nbytes(ws), _s(stream)))
@@ -504,6 +543,7 @@ def hl_embbag_bwd_clip(h, w_hot, staging, staging_rows, n_samples, bags_per_samp
     _check_plain(sq, "float64", 1, "sq")
     if norm_out is not None:
         _check_plain(norm_out, "float32", 1, "norm_out")
+    _check_gpu(h, "hl_embbag_bwd_clip", w_hot, staging, sq, ws, norm_out)
     _ck("hl_embbag_bwd_clip", lib().hl_embbag_bwd_clip(
         h.ptr, _p(w_hot), _p(staging), int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(sq),
         sq.numel(), float(max_norm), float(lr), _p(ws), _nbytes(ws), _p(norm_out), _s(stream)))
@@ -552,6 +592,7 @@ class Route:
             _check_plain(order, "int32", n_rows, "order")
         self.n_tokens, self.k, self.n_experts, self.n_rows = int(n_tokens), int(k), int(n_experts), int(n_rows)
         self.counts, self.offsets, self.pos, self.order = counts, offsets, pos, order
+        self.gpu = _gpu_of((counts, offsets, pos, order))
         self.struct = RouteStruct(self.n_tokens, self.k, self.n_experts, int(capacity), int(align), self.n_rows,
                                   _p(counts), _p(offsets), _p(pos), _p(order))
         self.ref = C.byref(self.struct)
@@ -573,29 +614,37 @@ def _weights_arg(w, route, what):
 
 def hl_route_plan(h, route, experts, ws=None, stream=None):
     _check_plain(experts, "int32", route.n_tokens * route.k, "experts")
+    _check_held(h, route, "route")
+    _check_gpu(h, "hl_route_plan", experts, ws)
     _ck("hl_route_plan", lib().hl_route_plan(h.ptr, route.ref, experts.data_ptr(), _p(ws),
                                              0 if ws is None else _nbytes(ws), _s(stream)))
 
 
 def hl_route_gather(h, route, x, rows, stream=None):
     dt, d = x.dtype, x.shape[-1]
-    xs, rs = _rows_arg(x, route.n_tokens, dt, d, "x"), _rows_arg(rows, route.n_rows, dt, d, "rows")
-    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, route.ref, _dt(x), d, x.data_ptr(), xs, rows.data_ptr(), rs,
+    xs, rs, code = _rows_arg(x, route.n_tokens, dt, d, "x"), _rows_arg(rows, route.n_rows, dt, d, "rows"), _dt(x)
+    _check_held(h, route, "route")
+    _check_gpu(h, "hl_route_gather", x, rows)
+    _ck("hl_route_gather", lib().hl_route_gather(h.ptr, route.ref, code, d, x.data_ptr(), xs, rows.data_ptr(), rs,
                                                  _s(stream)))
 
 
 def hl_route_gather_bwd(h, route, drows, dx, stream=None):
     dt, d = drows.dtype, drows.shape[-1]
-    rs, xs = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx")
-    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, _dt(drows), d, drows.data_ptr(), rs,
+    rs, xs, code = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx"), _dt(drows)
+    _check_held(h, route, "route")
+    _check_gpu(h, "hl_route_gather_bwd", drows, dx)
+    _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, code, d, drows.data_ptr(), rs,
                                                          dx.data_ptr(), xs, _s(stream)))
 
 
 def hl_route_combine(h, route, rows, weights, out, stream=None):
     dt, d = rows.dtype, rows.shape[-1]
-    rs, os_ = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out")
+    rs, os_, code = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out"), _dt(rows)
     _weights_arg(weights, route, "weights")
-    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, route.ref, _dt(rows), d, rows.data_ptr(), rs, _p(weights),
+    _check_held(h, route, "route")
+    _check_gpu(h, "hl_route_combine", rows, weights, out)
+    _ck("hl_route_combine", lib().hl_route_combine(h.ptr, route.ref, code, d, rows.data_ptr(), rs, _p(weights),
                                                    out.data_ptr(), os_, _s(stream)))
 
 
@@ -603,11 +652,13 @@ def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, st
     """rows may be None where dweights is."""
     dt, d = dout.dtype, dout.shape[-1]
     ds, drs = _rows_arg(dout, route.n_tokens, dt, d, "dout"), _rows_arg(drows, route.n_rows, dt, d, "drows")
-    rs = 0 if rows is None else _rows_arg(rows, route.n_rows, dt, d, "rows")
+    rs, code = 0 if rows is None else _rows_arg(rows, route.n_rows, dt, d, "rows"), _dt(dout)
     _weights_arg(weights, route, "weights")
     _weights_arg(dweights, route, "dweights")
+    _check_held(h, route, "route")
+    _check_gpu(h, "hl_route_combine_bwd", dout, rows, weights, drows, dweights)
     _ck("hl_route_combine_bwd", lib().hl_route_combine_bwd(
-        h.ptr, route.ref, _dt(dout), d, dout.data_ptr(), ds, _p(rows), rs, _p(weights), drows.data_ptr(), drs,
+        h.ptr, route.ref, code, d, dout.data_ptr(), ds, _p(rows), rs, _p(weights), drows.data_ptr(), drs,
         _p(dweights), _s(stream)))
 
 
@@ -622,6 +673,7 @@ class GradList:
         dst = self.grads if self.out is None else self.out
         if len(dst) != len(self.grads):
             raise ValueError(f"{len(self.grads)} gradients, {len(dst)} outputs")
+        self.gpu = _gpu_of(self.grads if self.out is None else self.grads + self.out)
         self.array = (GradStruct * max(1, len(self.grads)))()
         for a, g, d in zip(self.array, self.grads, dst):
             if not g.is_contiguous() or not d.is_contiguous() or d.dtype != g.dtype or d.numel() != g.numel():
@@ -652,6 +704,8 @@ def hl_grad_workspace_bytes():
 def hl_grad_sq(h, grads, sq, ws, stream=None):
     """grads: a GradList; sq: a float64 tensor, its first entry written."""
     _check_plain(sq, "float64", 1, "sq")
+    _check_held(h, grads, "grads")
+    _check_gpu(h, "hl_grad_sq", sq, ws)
     _ck("hl_grad_sq", lib().hl_grad_sq(h.ptr, grads.array, len(grads), _p(sq), _p(ws), _nbytes(ws), _s(stream)))
 
 
@@ -660,6 +714,8 @@ def hl_grad_clip(h, grads, sq, max_norm, norm_out=None, stream=None):
     _check_plain(sq, "float64", 1, "sq")
     if norm_out is not None:
         _check_plain(norm_out, "float32", 1, "norm_out")
+    _check_held(h, grads, "grads")
+    _check_gpu(h, "hl_grad_clip", sq, norm_out)
     _ck("hl_grad_clip", lib().hl_grad_clip(h.ptr, grads.array, len(grads), _p(sq), sq.numel(), float(max_norm),
                                            _p(norm_out), _s(stream)))
 
