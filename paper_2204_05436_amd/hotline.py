@@ -7,6 +7,7 @@ from __future__ import annotations
 import atexit
 import ctypes as C
 import itertools
+import operator
 import os
 import sys
 
@@ -295,10 +296,24 @@ def hl_status_string(status):
     return lib().hl_status_string(status).decode()
 
 
+_names = {"f32": HL_F32, "float32": HL_F32, "bf16": HL_BF16, "bfloat16": HL_BF16, "f16": HL_F16, "float16": HL_F16}
+
+
+def _row_type(dtype):
+    """The hl_dtype that a name, a torch type or one of its numbers stands for (the library takes f32 and bf16)."""
+    dt = _names.get(str(dtype).removeprefix("torch."))
+    if dt is None:
+        try:
+            dt = operator.index(dtype)
+        except TypeError:
+            raise ValueError(f"dtype: \"f32\" or \"bf16\" wanted, got {dtype!r}") from None
+    return dt
+
+
 def hl_create(rows_per_table, dim, dtype, k_cap):
     rows = np.ascontiguousarray(rows_per_table, dtype=np.uint32)
     h = P()
-    dt = HL_F32 if dtype in ("f32", HL_F32) else HL_BF16
+    dt = _row_type(dtype)
     _ck("hl_create", lib().hl_create(C.byref(h), len(rows), rows.ctypes.data, int(dim), dt, int(k_cap)))
     import torch
     return Handle(h.value, torch.cuda.current_device(), int(dim))
@@ -631,7 +646,8 @@ def hl_route_gather(h, route, x, rows, stream=None):
 
 def hl_route_gather_bwd(h, route, drows, dx, stream=None):
     dt, d = drows.dtype, drows.shape[-1]
-    rs, xs, code = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx"), _dt(drows)
+    rs, xs = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx")
+    code = _dt(drows)
     _check_held(h, route, "route")
     _check_gpu(h, "hl_route_gather_bwd", drows, dx)
     _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, code, d, drows.data_ptr(), rs,
@@ -640,7 +656,8 @@ def hl_route_gather_bwd(h, route, drows, dx, stream=None):
 
 def hl_route_combine(h, route, rows, weights, out, stream=None):
     dt, d = rows.dtype, rows.shape[-1]
-    rs, os_, code = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out"), _dt(rows)
+    rs, os_ = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out")
+    code = _dt(rows)
     _weights_arg(weights, route, "weights")
     _check_held(h, route, "route")
     _check_gpu(h, "hl_route_combine", rows, weights, out)
