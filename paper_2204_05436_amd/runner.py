@@ -233,9 +233,17 @@ class HotPath:
         if next is not None and mode != "pipelined":
             raise ValueError("look-ahead needs the native pipelined step")
         if max_norm is not None and mode != "sequential":
-            raise ValueError("clipping needs every gradient before the first update: mode \"sequential\"")
+            raise ValueError("only mode \"sequential\" has the clipped update")
         if norm_parts is not None and max_norm is None:
             raise ValueError("norm_parts without max_norm")
+        if max_norm is not None:  # (before any part of the step runs)
+            if b.dY is None:
+                raise ValueError("max_norm without a gradient (dY)")
+            if not max_norm >= 0:
+                raise ValueError(f"max_norm: {max_norm}")
+            if norm_parts is not None:
+                hl._check_plain(norm_parts, "float64", 1, "norm_parts")
+                hl._check_gpu(self.h, "norm_parts", norm_parts)
         if mode == "sequential":
             return self._step_sequential(b, lr, events, split_fwd, max_norm, norm_parts)
         caller = torch.cuda.current_stream(self.device)
