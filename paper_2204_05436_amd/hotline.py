@@ -216,6 +216,21 @@ def _s(stream):
     return stream.cuda_stream
 
 
+_stream_on = None  # a device's current stream
+
+
+def _sh(h, stream):
+    """As _s, on the handle's GPU (for calls that demand that it is the current one: no need to ask which that is)."""
+    global _stream_on
+    if stream is None:
+        if _stream_on is None:
+            import torch
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            _stream_on = raw if raw else lambda device: torch.cuda.current_stream(device).cuda_stream
+        return _stream_on(h.device)
+    return _s(stream)
+
+
 def _nbytes(t):
     return t.numel() * t.element_size()
 
@@ -260,10 +275,11 @@ def _check_gpu(h, what, *tensors):
         raise ValueError(f"{what}: tensors on the handle's GPU wanted (cuda:{gpu}), got one on {x.device}")
 
 
-def _check_held(h, held, what):
-    """As _check_gpu, for a Route or a GradList, which looked at its tensors when it was made."""
+def _check_held(h, held, what, *tensors):
+    """As _check_gpu, for a Route or a GradList too, which looked at its tensors when it was made."""
     if held.gpu is not None and held.gpu != h.device:
         raise ValueError(f"{what}: its tensors on the handle's GPU wanted (cuda:{h.device})")
+    _check_gpu(h, what, *tensors)
 
 
 class Handle:
@@ -549,7 +565,7 @@ def hl_embbag_bwd_norm(h, staging_rows, n_samples, bags_per_sample, n_lookups, d
     _check_gpu(h, "hl_embbag_bwd_norm", dY, sq, ws)
     _ck("hl_embbag_bwd_norm", lib().hl_embbag_bwd_norm(
         h.ptr, int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(dY), _p(sq), _p(ws),
-        _nbytes(ws), _s(stream)))
+        _nbytes(ws), _sh(h, stream)))
 
 
 def hl_embbag_bwd_clip(h, w_hot, staging, staging_rows, n_samples, bags_per_sample, n_lookups, sq, max_norm, lr, ws,
@@ -561,7 +577,7 @@ def hl_embbag_bwd_clip(h, w_hot, staging, staging_rows, n_samples, bags_per_samp
     _check_gpu(h, "hl_embbag_bwd_clip", w_hot, staging, sq, ws, norm_out)
     _ck("hl_embbag_bwd_clip", lib().hl_embbag_bwd_clip(
         h.ptr, _p(w_hot), _p(staging), int(staging_rows), int(n_samples), int(bags_per_sample), int(n_lookups), _p(sq),
-        sq.numel(), float(max_norm), float(lr), _p(ws), _nbytes(ws), _p(norm_out), _s(stream)))
+        sq.numel(), float(max_norm), float(lr), _p(ws), _nbytes(ws), _p(norm_out), _sh(h, stream)))
 
 
 # ------------------------------------------------------------------ routing
@@ -577,7 +593,9 @@ def _torch_types():
 
 def _dt(x):
     """The hl_dtype of a tensor (bf16 and fp16 by their torch types)."""
-    dt = _torch_types().get(x.dtype)
+    dt = _types.get(x.dtype)
+    if dt is None:
+        dt = _torch_types().get(x.dtype)
     if dt is None:
         raise TypeError(f"float32, bfloat16 or float16 wanted, got {x.dtype}")
     return dt
@@ -629,29 +647,32 @@ def _weights_arg(w, route, what):
 
 def hl_route_plan(h, route, experts, ws=None, stream=None):
     _check_plain(experts, "int32", route.n_tokens * route.k, "experts")
-    _check_held(h, route, "route")
-    _check_gpu(h, "hl_route_plan", experts, ws)
+    g = h.device  # (all of it there, or a closer look)
+    if not (route.gpu == g and experts.get_device() == g and (ws is None or ws.get_device() == g)):
+        _check_held(h, route, "hl_route_plan", experts, ws)
     _ck("hl_route_plan", lib().hl_route_plan(h.ptr, route.ref, experts.data_ptr(), _p(ws),
-                                             0 if ws is None else _nbytes(ws), _s(stream)))
+                                             0 if ws is None else _nbytes(ws), _sh(h, stream)))
 
 
 def hl_route_gather(h, route, x, rows, stream=None):
     dt, d = x.dtype, x.shape[-1]
     xs, rs, code = _rows_arg(x, route.n_tokens, dt, d, "x"), _rows_arg(rows, route.n_rows, dt, d, "rows"), _dt(x)
-    _check_held(h, route, "route")
-    _check_gpu(h, "hl_route_gather", x, rows)
+    g = h.device  # (all of it there, or a closer look)
+    if not (route.gpu == g and x.get_device() == g and rows.get_device() == g):
+        _check_held(h, route, "hl_route_gather", x, rows)
     _ck("hl_route_gather", lib().hl_route_gather(h.ptr, route.ref, code, d, x.data_ptr(), xs, rows.data_ptr(), rs,
-                                                 _s(stream)))
+                                                 _sh(h, stream)))
 
 
 def hl_route_gather_bwd(h, route, drows, dx, stream=None):
     dt, d = drows.dtype, drows.shape[-1]
     rs, xs = _rows_arg(drows, route.n_rows, dt, d, "drows"), _rows_arg(dx, route.n_tokens, dt, d, "dx")
     code = _dt(drows)
-    _check_held(h, route, "route")
-    _check_gpu(h, "hl_route_gather_bwd", drows, dx)
+    g = h.device  # (all of it there, or a closer look)
+    if not (route.gpu == g and drows.get_device() == g and dx.get_device() == g):
+        _check_held(h, route, "hl_route_gather_bwd", drows, dx)
     _ck("hl_route_gather_bwd", lib().hl_route_gather_bwd(h.ptr, route.ref, code, d, drows.data_ptr(), rs,
-                                                         dx.data_ptr(), xs, _s(stream)))
+                                                         dx.data_ptr(), xs, _sh(h, stream)))
 
 
 def hl_route_combine(h, route, rows, weights, out, stream=None):
@@ -659,10 +680,12 @@ def hl_route_combine(h, route, rows, weights, out, stream=None):
     rs, os_ = _rows_arg(rows, route.n_rows, dt, d, "rows"), _rows_arg(out, route.n_tokens, dt, d, "out")
     code = _dt(rows)
     _weights_arg(weights, route, "weights")
-    _check_held(h, route, "route")
-    _check_gpu(h, "hl_route_combine", rows, weights, out)
+    g = h.device  # (all of it there, or a closer look)
+    if not (route.gpu == g and rows.get_device() == g and out.get_device() == g and
+            (weights is None or weights.get_device() == g)):
+        _check_held(h, route, "hl_route_combine", rows, weights, out)
     _ck("hl_route_combine", lib().hl_route_combine(h.ptr, route.ref, code, d, rows.data_ptr(), rs, _p(weights),
-                                                   out.data_ptr(), os_, _s(stream)))
+                                                   out.data_ptr(), os_, _sh(h, stream)))
 
 
 def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, stream=None):
@@ -672,11 +695,14 @@ def hl_route_combine_bwd(h, route, dout, rows, weights, drows, dweights=None, st
     rs, code = 0 if rows is None else _rows_arg(rows, route.n_rows, dt, d, "rows"), _dt(dout)
     _weights_arg(weights, route, "weights")
     _weights_arg(dweights, route, "dweights")
-    _check_held(h, route, "route")
-    _check_gpu(h, "hl_route_combine_bwd", dout, rows, weights, drows, dweights)
+    g = h.device  # (all of it there, or a closer look)
+    if not (route.gpu == g and dout.get_device() == g and drows.get_device() == g and
+            (rows is None or rows.get_device() == g) and (weights is None or weights.get_device() == g) and
+            (dweights is None or dweights.get_device() == g)):
+        _check_held(h, route, "hl_route_combine_bwd", dout, rows, weights, drows, dweights)
     _ck("hl_route_combine_bwd", lib().hl_route_combine_bwd(
         h.ptr, route.ref, code, d, dout.data_ptr(), ds, _p(rows), rs, _p(weights), drows.data_ptr(), drs,
-        _p(dweights), _s(stream)))
+        _p(dweights), _sh(h, stream)))
 
 
 # ------------------------------------------------------------------ clipping
@@ -721,9 +747,10 @@ def hl_grad_workspace_bytes():
 def hl_grad_sq(h, grads, sq, ws, stream=None):
     """grads: a GradList; sq: a float64 tensor, its first entry written."""
     _check_plain(sq, "float64", 1, "sq")
-    _check_held(h, grads, "grads")
-    _check_gpu(h, "hl_grad_sq", sq, ws)
-    _ck("hl_grad_sq", lib().hl_grad_sq(h.ptr, grads.array, len(grads), _p(sq), _p(ws), _nbytes(ws), _s(stream)))
+    g = h.device  # (all of it there, or a closer look)
+    if not (grads.gpu == g and sq.get_device() == g and ws.get_device() == g):
+        _check_held(h, grads, "hl_grad_sq", sq, ws)
+    _ck("hl_grad_sq", lib().hl_grad_sq(h.ptr, grads.array, len(grads), _p(sq), _p(ws), _nbytes(ws), _sh(h, stream)))
 
 
 def hl_grad_clip(h, grads, sq, max_norm, norm_out=None, stream=None):
@@ -731,10 +758,11 @@ def hl_grad_clip(h, grads, sq, max_norm, norm_out=None, stream=None):
     _check_plain(sq, "float64", 1, "sq")
     if norm_out is not None:
         _check_plain(norm_out, "float32", 1, "norm_out")
-    _check_held(h, grads, "grads")
-    _check_gpu(h, "hl_grad_clip", sq, norm_out)
+    g = h.device  # (all of it there, or a closer look)
+    if not (grads.gpu == g and sq.get_device() == g and (norm_out is None or norm_out.get_device() == g)):
+        _check_held(h, grads, "hl_grad_clip", sq, norm_out)
     _ck("hl_grad_clip", lib().hl_grad_clip(h.ptr, grads.array, len(grads), _p(sq), sq.numel(), float(max_norm),
-                                           _p(norm_out), _s(stream)))
+                                           _p(norm_out), _sh(h, stream)))
 
 
 def hl_debug_ballot_ranks(h, on):
