@@ -718,16 +718,20 @@ class GradList:
             raise ValueError(f"{len(self.grads)} gradients, {len(dst)} outputs")
         self.gpu = _gpu_of(self.grads if self.out is None else self.grads + self.out)
         self.array = (GradStruct * max(1, len(self.grads)))()
-        for a, g, d in zip(self.array, self.grads, dst):
-            if not g.is_contiguous() or not d.is_contiguous() or d.dtype != g.dtype or d.numel() != g.numel():
-                raise ValueError("gradients and their outputs: contiguous, of the same type and size")
-            a.src, a.dst, a.n, a.dtype = _p(g), _p(d), g.numel(), _dt(g)
         # an output that another entry reads or writes would be scaled before, after or twice
         spans = []
-        for a in self.array[:len(self.grads)]:
-            size = a.n * (4 if a.dtype == HL_F32 else 2)
-            for p in {a.src, a.dst} if size else ():
-                spans.append((p, p + size, p == a.dst))
+        for a, g, d in zip(self.array, self.grads, dst):
+            n, src = g.numel(), g.data_ptr()
+            same = d is g or (d.is_contiguous() and d.dtype == g.dtype and d.numel() == n)
+            if not g.is_contiguous() or not same:
+                raise ValueError("gradients and their outputs: contiguous, of the same type and size")
+            to, dt = src if d is g else d.data_ptr(), _dt(g)
+            a.src, a.dst, a.n, a.dtype = src, to, n, dt
+            if n:
+                size = n * (4 if dt == HL_F32 else 2)
+                spans.append((to, to + size, True))
+                if src != to:
+                    spans.append((src, src + size, False))
         end = written = 0  # the furthest end so far, of all and of outputs
         for lo, hi, out in sorted(spans):
             if lo < (end if out else written):
