@@ -725,10 +725,10 @@ bw_norm2(uint32_t n_tiles, eb_geom g, const float* __restrict__ tfirst, const fl
 // one (BW_NORM above; E positions per group) applies row <- round(row - lr * G), lr
 // scaled by the clipping coefficient.  A wave tests BC_POS positions, lists those
 // found in LDS, and its row groups take them RPG at a time, all loads in flight
-// together.  Bound by the rows and sums, each read once: 213,000 lookups of f32 rows
-// of 64 11.0 us, 328,000 of bf16 rows of 128 15.9.  (Before the factor's exponent
-// came in, 16 positions 10.2 and 15.1, 8 12.1 and 19.0, 32 11.8 and 17.1, 64 18.0 and
-// 21.9; 2 rows in flight 10.9 and 15.1.)
+// together.  213,000 lookups of f32 rows of 64 take 10.9 us, 328,000 of bf16 rows of
+// 128 16.3, for 36 and 58 MB: bound by the latency of key, list and row, since 16
+// positions hold only 3 or 4 rows there.  (8 positions 12.9 and 18.5, 32 12.8 and 17.2,
+// 64 18.0 and 22.3; 2 rows in flight 11.7 and 16.5.)
 #define BC_POS 16
 template <int VEC, bool BF>
 __global__ void __launch_bounds__(256)
@@ -1412,7 +1412,7 @@ hl_status hl_embbag_bwd_apply_any(hl_handle* h, void* w_hot, void* staging, int3
 }
 
 // What the two halves of the clipped update share: the plan's record, its
-// workspace and its sorted pairs (pass: the record's state that the call needs).
+// workspace and its sorted pairs.
 static hl_status norm_setup(hl_handle* h, int32_t stg_rows, int32_t n_samples, int32_t bps, int64_t n_lookups,
                             void* workspace, size_t ws_bytes, hl_ws_rec** rec, bw_ws* ws, uint32_t** sk,
                             uint32_t** sv) {
