@@ -558,7 +558,7 @@ def hl_embbag_bwd_grouping(h, staging_rows, n_samples, bags_per_sample, n_lookup
 
 
 def hl_embbag_bwd_norm(h, staging_rows, n_samples, bags_per_sample, n_lookups, dY, sq, ws, stream=None):
-    """sq: a float64 tensor, its first entry written."""
+    """dY: n_samples * bags_per_sample rows of dim contiguous fp32; sq: a float64 tensor, its first entry written."""
     _check_plain(sq, "float64", 1, "sq")
     if dY is not None and not isinstance(dY, int):
         _check_plain(dY, "float32", n_samples * bags_per_sample * h.dim, "dY")

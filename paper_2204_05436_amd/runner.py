@@ -221,9 +221,10 @@ class HotPath:
           `events`: optional list of len(STAGES)+1 torch.cuda.Event recorded
           around the stages.  max_norm: the update is clipped by the step's
           gradient norm (hl_embbag_bwd_norm, hl_embbag_bwd_clip), which
-          self.grad_norm receives; norm_parts: the norm's parts, a float64
-          tensor whose first entry receives the tables' part and whose others
-          hold the rest of the model's (hl_grad_sq; none by default).
+          self.grad_norm receives (a batch without dY is refused);
+          norm_parts: the norm's parts, a float64 tensor whose first entry
+          receives the tables' part and whose others hold the rest of the
+          model's (hl_grad_sq; none by default).
         mode "fwdbwd": as pipelined, but the fetch is awaited before the
           forward/backward section, which `events` (two events) brackets."""
         if mode not in MODES:
